@@ -395,6 +395,81 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
                       int32_t b, int32_t k, uint16_t* loss, uint16_t* dlogits, uint16_t* dbias,
                       void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------- orthogonalised updates
+ * Orthogonalisation of gradient matrices by Newton-Schulz products, and the
+ * optimiser step around it (Muon): an alternative to pf16_sgd_update for the
+ * weights that are matrices -- a convolution's filter as [k][r*s*c], the
+ * classifier as [k][c].  No counterpart in the paper, whose update is SGD.
+ *
+ * For each matrix u of rows x cols (either may be larger):
+ *   X = u / |u|_F;  `steps` times:  S = X X^T,  X = a X + (b S + c S S) X,
+ *   (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * whose result has u's singular vectors and, after five steps, singular values
+ * between 0.68 and 1.21 for all but the smallest.  X is held in FP32; the
+ * products take binary16 copies (scaled by powers of two) and accumulate in
+ * FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
+ * norm is not finite gives NaNs throughout.  Same inputs, same bits.
+ *
+ * All matrices of one call run together, in two launches.  1 <= rows, cols <=
+ * 65536, rows * cols <= 2^30, at most PF16_ORTHO_MAX_MATRICES matrices
+ * (PF16_ERR_UNSUPPORTED beyond), 1 <= steps <= 16 (PF16_ERR_ARG).  The list
+ * is host memory, read before the call returns.  Arrays are dense, row-major,
+ * 16-byte aligned, and so is the workspace.  count may be 0 (nothing is
+ * launched). */
+#define PF16_ORTHO_MAX_MATRICES 256
+typedef struct {
+  const uint16_t* g; /* [rows][cols] */
+  uint16_t* o;       /* [rows][cols], the result; may be g itself, else it overlaps no array of the call
+                        (PF16_ERR_ARG) */
+  int32_t rows, cols;
+} pf16_ortho_matrix;
+/* Bytes of workspace; 0 for an invalid list as well (the call then reports the error). */
+size_t pf16_ortho_workspace_size(const pf16_ortho_matrix* mats, int32_t count);
+int pf16_orthogonalize(const pf16_ortho_matrix* mats, int32_t count, int32_t steps, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* One step of the optimiser, in place on w and v (start v at +0):
+ *   v = rn(momentum*v + g)
+ *   u = g + momentum*v  with PF16_MUON_NESTEROV, else v   (v as stored)
+ *   w = rn(w - lr*(scale*O(u) + wd*w)),  O(u) the result above, unrounded
+ * with everything between the stored tensors in FP32.  lr, momentum and wd
+ * are finite floats, scale too (per matrix: often sqrt(max(1, rows/cols)))
+ * (PF16_ERR_ARG).  w and v overlap nothing else of the call (PF16_ERR_ARG). */
+#define PF16_MUON_NESTEROV 0x1u
+typedef struct {
+  uint16_t* w;       /* [rows][cols] */
+  uint16_t* v;       /* momentum */
+  const uint16_t* g; /* gradient */
+  int32_t rows, cols;
+  float scale;
+} pf16_muon_matrix;
+size_t pf16_muon_workspace_size(const pf16_muon_matrix* mats, int32_t count);
+int pf16_muon_update(const pf16_muon_matrix* mats, int32_t count, float lr, float momentum, float wd, int32_t steps,
+                     uint32_t flags, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------- linear layers in 8-bit integers
+ * The classifier, or a 1x1 convolution over its pixels, for answering with a
+ * trained network: rows of x (one per token or pixel) and of w (one per output
+ * channel) as 8-bit integers with one FP32 scale each.  No counterpart in the
+ * paper.
+ *
+ * Quantisation of the rows of x[m][k], with A_i = max_k |x[i][k]|:
+ *   scale[i] = A_i / 127,  q[i][k] = rint(127 x[i][k] / A_i)
+ * the quotient as a real number, ties to even: |q| <= 127 and some |q| of each
+ * row is 127.  A zero row has scale 0 and zeros; a row with an infinity or a
+ * NaN has scale NaN and zeros, so that every product with it is NaN.  m may
+ * be 0.  k >= 1; x and q 16-byte aligned, scale 4-byte; the three do not overlap
+ * (PF16_ERR_ARG). */
+int pf16_quantize_i8(const uint16_t* x, int8_t* q, float* scale, int32_t m, int32_t k, void* stream);
+/* y[i][j] = rn(sx[i]*sw[j] * sum_k x[i][k] w[j][k] + bias[j]), bias binary16
+ * or NULL.  The integer sum is exact up to k = 1024, and for any k while its
+ * partial sums stay within 2^24; beyond, partial sums are FP32.  The scale
+ * and the bias are applied in FP32 and the result is rounded once.  Any values
+ * of x and w, -128 included.  m may be 0; n, k >= 1; k <= 65536.  x, w and y
+ * 16-byte aligned, sx and sw 4-byte, bias 2-byte; y overlaps nothing else (PF16_ERR_ARG). */
+int pf16_linear_i8(const int8_t* x, const float* sx, const int8_t* w, const float* sw, const uint16_t* bias,
+                   uint16_t* y, int32_t m, int32_t n, int32_t k, void* stream);
+
 /* --------------------------------------------------------------- status
  * Waits for `stream`, then returns and clears the device status word of the
  * current device: PF16_OK, PF16_ERR_TIMEOUT after a bounded wait ran out, or

@@ -6,12 +6,15 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <mutex>
 
 #include "../../include/pf16.h"
+#include "pf16_int8.h"
 #include "pf16_internal.h"
+#include "pf16_ortho.h"
 #include "pf16_ptx.cuh"
 
 namespace pf16 {
@@ -1640,6 +1643,215 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
                  cudaSuccess
              ? PF16_OK
              : PF16_ERR_CUDA;
+}
+
+// ------------------------------------------------- orthogonalised updates
+// A list of matrices checked and laid out in the workspace: header (counters,
+// partial sums), then each matrix's buffers.  Matrices are ordered by the work
+// of one tile, longest first, so that no long one is left for a phase's end.
+struct OrthoEntry {
+  const uint16_t* g;
+  uint16_t *v, *w;
+  int rows, cols;
+  float scale;
+};
+
+static int ortho_shape(int rows, int cols) {
+  if (rows <= 0 || cols <= 0) return PF16_ERR_SHAPE;
+  if (rows > 65536 || cols > 65536 || (long long)rows * cols > (1ll << 30)) return PF16_ERR_SHAPE;
+  return PF16_OK;
+}
+
+static int ortho_parts(long long numel) {
+  return (int)std::min<long long>(kOrthoMaxParts, (numel + 8191) / 8192);
+}
+
+// Fills p's lists and returns the bytes of workspace (base may be null).
+static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t* base) {
+  int order[kOrthoMax];
+  for (int i = 0; i < count; ++i) order[i] = i;
+  std::sort(order, order + count, [&](int a, int b) {
+    const int la = std::max(e[a].rows, e[a].cols), lb = std::max(e[b].rows, e[b].cols);
+    return la != lb ? la > lb : a < b;
+  });
+  p->count = count;
+  p->ticket = reinterpret_cast<uint32_t*>(base);
+  p->done = p->ticket + 4;
+  size_t at = round_up(16 + (size_t)count * 4, 256);
+  p->parts = reinterpret_cast<float*>(base + at);
+  long long parts = 0, pack = 0, sym = 0, full = 0;
+  for (int i = 0; i < count; ++i) {
+    const OrthoEntry& s = e[order[i]];
+    OrthoMat& m = p->mat[i];
+    m.g = s.g;
+    m.v = s.v;
+    m.w = s.w;
+    m.rows = s.rows;
+    m.cols = s.cols;
+    m.scale = s.scale;
+    m.tall = s.rows > s.cols;
+    m.mb = cdiv(std::min(s.rows, s.cols), 64);
+    m.nb = cdiv(std::max(s.rows, s.cols), 64);
+    m.part0 = (int)parts;
+    m.parts = ortho_parts((long long)s.rows * s.cols);
+    parts += m.parts;
+    const int mt = cdiv(m.mb, 2), nt = cdiv(m.nb, 2);
+    p->pre_pack[i] = (int)pack;
+    p->pre_sym[i] = (int)sym;
+    p->pre_full[i] = (int)full;
+    pack += (long long)m.mb * m.nb;
+    sym += (long long)mt * (mt + 1) / 2;
+    full += (long long)mt * nt;
+  }
+  p->pre_pack[count] = (int)pack;
+  p->pre_sym[count] = (int)sym;
+  p->pre_full[count] = (int)full;
+  p->total_parts = (int)parts;
+  p->max_items = (int)std::max(std::max(pack, sym), full);
+  at += round_up((size_t)parts * 4, 256);
+  for (int i = 0; i < count; ++i) {
+    p->mat[i].ws = base + at;
+    at += ortho_layout(p->mat[i].mb, p->mat[i].nb).bytes;
+  }
+  return at;
+}
+
+// Entries of a C list, after its checks; `o` distinguishes the two element types.
+static int ortho_entries(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int count, OrthoEntry* e) {
+  if (count < 0) return PF16_ERR_SHAPE;
+  if (count > PF16_ORTHO_MAX_MATRICES) return PF16_ERR_UNSUPPORTED;
+  if (count > 0 && !o && !u) return PF16_ERR_NULL;
+  for (int i = 0; i < count; ++i) {
+    if (o)
+      e[i] = OrthoEntry{o[i].g, nullptr, o[i].o, o[i].rows, o[i].cols, 1.f};
+    else
+      e[i] = OrthoEntry{u[i].g, u[i].v, u[i].w, u[i].rows, u[i].cols, u[i].scale};
+    const int rc = ortho_shape(e[i].rows, e[i].cols);
+    if (rc != PF16_OK) return rc;
+  }
+  return PF16_OK;
+}
+
+// Pointers, and that no written array meets another array of the call or the workspace.
+static int ortho_pointers(const OrthoEntry* e, int count, bool muon, const void* ws, size_t ws_bytes, size_t need) {
+  struct Range {
+    uintptr_t lo, hi;
+    bool written;
+  };
+  Range r[3 * kOrthoMax + 1];
+  int n = 0;
+  for (int i = 0; i < count; ++i) {
+    if (!e[i].g || !e[i].w || (muon && !e[i].v)) return PF16_ERR_NULL;
+    if (!aligned16(e[i].g) || !aligned16(e[i].w) || (muon && !aligned16(e[i].v))) return PF16_ERR_ALIGN;
+    const size_t bytes = (size_t)e[i].rows * e[i].cols * 2;
+    auto add = [&](const void* p, bool written) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+      r[n++] = Range{a, a + bytes, written};
+    };
+    add(e[i].w, true);
+    if (muon) add(e[i].v, true);
+    if (muon || e[i].g != e[i].w) add(e[i].g, false);  // (an output may be its own input)
+  }
+  if (!ws || ws_bytes < need) return PF16_ERR_WORKSPACE;
+  if (!aligned16(ws)) return PF16_ERR_ALIGN;
+  r[n++] = Range{reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + need, true};
+  std::sort(r, r + n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  uintptr_t any = 0, written = 0;  // the furthest ends so far
+  for (int i = 0; i < n; ++i) {
+    if (r[i].lo < written || (r[i].written && r[i].lo < any)) return PF16_ERR_ARG;
+    any = std::max(any, r[i].hi);
+    if (r[i].written) written = std::max(written, r[i].hi);
+  }
+  return PF16_OK;
+}
+
+static size_t ortho_ws(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int32_t count) {
+  OrthoEntry e[kOrthoMax];
+  if (ortho_entries(o, u, count, e) != PF16_OK || count == 0) return 0;
+  OrthoParams p;
+  return ortho_plan(&p, e, count, nullptr);
+}
+
+static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int32_t count, int32_t steps, float lr,
+                     float momentum, float wd, bool nesterov, void* ws, size_t ws_bytes, void* stream) {
+  OrthoEntry e[kOrthoMax];
+  int rc = ortho_entries(o, u, count, e);
+  if (rc != PF16_OK) return rc;
+  if (steps < 1 || steps > 16) return PF16_ERR_ARG;
+  if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(wd)) return PF16_ERR_ARG;
+  for (int i = 0; i < count; ++i)
+    if (!std::isfinite(e[i].scale)) return PF16_ERR_ARG;
+  if (count == 0) return PF16_OK;
+  OrthoParams p;
+  const size_t need = ortho_plan(&p, e, count, static_cast<uint8_t*>(ws));
+  rc = ortho_pointers(e, count, u != nullptr, ws, ws_bytes, need);
+  if (rc != PF16_OK) return rc;
+  p.steps = steps;
+  p.muon = u != nullptr;
+  p.nesterov = nesterov;
+  p.lr = lr;
+  p.momentum = momentum;
+  p.wd = wd;
+  p.wait_limit_ns = 4000000000ull;
+  int sms;
+  rc = device_consts(&p.status, &sms);
+  if (rc != PF16_OK) return rc;
+  return launch_ortho(p, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK : PF16_ERR_CUDA;
+}
+
+size_t pf16_ortho_workspace_size(const pf16_ortho_matrix* mats, int32_t count) { return ortho_ws(mats, nullptr, count); }
+int pf16_orthogonalize(const pf16_ortho_matrix* mats, int32_t count, int32_t steps, void* ws, size_t ws_bytes,
+                       void* stream) {
+  return ortho_run(mats, nullptr, count, steps, 0.f, 0.f, 0.f, false, ws, ws_bytes, stream);
+}
+size_t pf16_muon_workspace_size(const pf16_muon_matrix* mats, int32_t count) { return ortho_ws(nullptr, mats, count); }
+int pf16_muon_update(const pf16_muon_matrix* mats, int32_t count, float lr, float momentum, float wd, int32_t steps,
+                     uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  if (flags & ~(uint32_t)PF16_MUON_NESTEROV) return PF16_ERR_ARG;
+  if (count > 0 && !mats) return PF16_ERR_NULL;
+  static const pf16_muon_matrix none = {};
+  return ortho_run(nullptr, mats ? mats : &none, count, steps, lr, momentum, wd, (flags & PF16_MUON_NESTEROV) != 0, ws,
+                   ws_bytes, stream);
+}
+
+// ------------------------------------------- linear layers in 8-bit integers
+static bool ranges_meet(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + bn && y < x + an;
+}
+
+int pf16_quantize_i8(const uint16_t* x, int8_t* q, float* scale, int32_t m, int32_t k, void* stream) {
+  if (m < 0 || k < 1) return PF16_ERR_SHAPE;
+  if (m == 0) return PF16_OK;
+  if (!x || !q || !scale) return PF16_ERR_NULL;
+  if (!aligned16(x) || !aligned16(q) || (reinterpret_cast<uintptr_t>(scale) & 3u)) return PF16_ERR_ALIGN;
+  const size_t n = (size_t)m * k;
+  if (ranges_meet(x, 2 * n, q, n) || ranges_meet(x, 2 * n, scale, (size_t)m * 4) ||
+      ranges_meet(q, n, scale, (size_t)m * 4))
+    return PF16_ERR_ARG;
+  return launch_quantize_i8(x, q, scale, m, k, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK
+                                                                                                  : PF16_ERR_CUDA;
+}
+
+int pf16_linear_i8(const int8_t* x, const float* sx, const int8_t* w, const float* sw, const uint16_t* bias,
+                   uint16_t* y, int32_t m, int32_t n, int32_t k, void* stream) {
+  if (m < 0 || n < 1 || k < 1 || k > 65536) return PF16_ERR_SHAPE;
+  if (m == 0) return PF16_OK;
+  if (!x || !sx || !w || !sw || !y) return PF16_ERR_NULL;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(y) || (reinterpret_cast<uintptr_t>(sx) & 3u) ||
+      (reinterpret_cast<uintptr_t>(sw) & 3u) || (reinterpret_cast<uintptr_t>(bias) & 1u))
+    return PF16_ERR_ALIGN;
+  const size_t yb = (size_t)m * n * 2;
+  if (ranges_meet(y, yb, x, (size_t)m * k) || ranges_meet(y, yb, w, (size_t)n * k) ||
+      ranges_meet(y, yb, sx, (size_t)m * 4) || ranges_meet(y, yb, sw, (size_t)n * 4) ||
+      (bias && ranges_meet(y, yb, bias, (size_t)n * 2)))
+    return PF16_ERR_ARG;
+  int* status;
+  int sms;
+  const int rc = device_consts(&status, &sms);
+  if (rc != PF16_OK) return rc;
+  const LinearI8 a{x, sx, w, sw, bias, y, m, n, k};
+  return launch_linear_i8(a, sms, status, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK : PF16_ERR_CUDA;
 }
 
 int pf16_sync_status(void* stream) {

@@ -1,0 +1,22 @@
+// Linear layers in 8-bit integers (pf16_int8.cu): what the C-ABI layer hands to the kernels.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+namespace pf16 {
+
+// y[m][n] = rn16(sx[i] * sw[j] * sum_k x[i][k] w[j][k] + bias[j])
+struct LinearI8 {
+  const int8_t* x;
+  const float* sx;
+  const int8_t* w;
+  const float* sw;
+  const uint16_t* bias;  // or null
+  uint16_t* y;
+  int m, n, k;
+};
+
+cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s);
+cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s);
+
+}  // namespace pf16

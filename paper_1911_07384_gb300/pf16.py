@@ -27,6 +27,8 @@ PF16_F32_ACCUM = 0x4
 PF16_BN_RELU = 0x1
 PF16_BN_RESIDUAL = 0x2
 PF16_BN_SWAP = 0x4
+PF16_MUON_NESTEROV = 0x1
+PF16_ORTHO_MAX_MATRICES = 256
 PF16_PASS_FWD, PF16_PASS_DGRAD, PF16_PASS_WGRAD = 0, 1, 2
 
 EXPORTS = [
@@ -39,6 +41,8 @@ EXPORTS = [
     "pf16_conv_bnstats_size", "pf16_conv_fwd_bnstats", "pf16_conv_dgrad_bnstats_size",
     "pf16_conv_dgrad_bnstats", "pf16_conv_dgrad_bnstats_add", "pf16_tc_rate", "pf16_wait_flag",
     "pf16_conv_fwd_bnin", "pf16_conv_wgrad_bnin", "pf16_bn_relu_maxpool_fwd",
+    "pf16_ortho_workspace_size", "pf16_orthogonalize", "pf16_muon_workspace_size", "pf16_muon_update",
+    "pf16_quantize_i8", "pf16_linear_i8",
 ]
 
 
@@ -80,6 +84,17 @@ _BN_T = ("x", "gamma", "beta", "residual", "dy", "y_saved", "y", "mean", "invstd
 
 class BnTensors(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in _BN_T]
+
+
+class OrthoMatrix(ctypes.Structure):
+    """pf16_ortho_matrix"""
+    _fields_ = [("g", ctypes.c_void_p), ("o", ctypes.c_void_p), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32)]
+
+
+class MuonMatrix(ctypes.Structure):
+    """pf16_muon_matrix"""
+    _fields_ = [("w", ctypes.c_void_p), ("v", ctypes.c_void_p), ("g", ctypes.c_void_p), ("rows", ctypes.c_int32),
+                ("cols", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lock = threading.Lock()
@@ -147,6 +162,16 @@ def lib():
             L.pf16_softmax_xent_workspace_size.restype = sz
             L.pf16_softmax_xent.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
             L.pf16_softmax_xent.restype = I
+            f32 = ctypes.c_float
+            for nm, mat in (("ortho", OrthoMatrix), ("muon", MuonMatrix)):
+                size = getattr(L, f"pf16_{nm}_workspace_size")
+                size.argtypes, size.restype = [ctypes.POINTER(mat), i32], sz
+            L.pf16_orthogonalize.argtypes = [ctypes.POINTER(OrthoMatrix), i32, i32, vp, sz, vp]
+            L.pf16_muon_update.argtypes = [ctypes.POINTER(MuonMatrix), i32, f32, f32, f32, i32, u32, vp, sz, vp]
+            L.pf16_quantize_i8.argtypes = [vp, vp, vp, i32, i32, vp]
+            L.pf16_linear_i8.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp]
+            for nm in ("pf16_orthogonalize", "pf16_muon_update", "pf16_quantize_i8", "pf16_linear_i8"):
+                getattr(L, nm).restype = I
             L.pf16_sync_status.argtypes = [vp]
             L.pf16_sync_status.restype = I
             L.pf16_status_string.argtypes = [I]
@@ -371,6 +396,50 @@ def softmax_xent(logits, bias, labels, b, k, loss, dlogits, dbias, ws, stream=No
     _check(lib().pf16_softmax_xent(_ptr(logits), _ptr(bias), _ptr(labels), b, k, _ptr(loss),
                                    _ptr(dlogits), _ptr(dbias), _ptr(ws), _nbytes(ws),
                                    _stream(stream)), "pf16_softmax_xent")
+
+
+def ortho_list(matrices):
+    """The list of an orthogonalize call, built once and kept: (g, o, rows, cols) of each matrix."""
+    rows = [OrthoMatrix(_ptr(g), _ptr(o), r, c) for g, o, r, c in matrices]
+    return (OrthoMatrix * len(rows))(*rows)
+
+
+def ortho_workspace_size(mats) -> int:
+    return int(lib().pf16_ortho_workspace_size(mats, len(mats)))
+
+
+def orthogonalize(mats, ws, steps=5, stream=None):
+    """Each matrix g of an ortho_list orthogonalised by Newton-Schulz products into its o."""
+    _check(lib().pf16_orthogonalize(mats, len(mats), steps, _ptr(ws), _nbytes(ws), _stream(stream)),
+           "pf16_orthogonalize")
+
+
+def muon_list(matrices):
+    """The list of a muon_update call, built once and kept: (w, v, g, rows, cols, scale) of each matrix."""
+    rows = [MuonMatrix(_ptr(w), _ptr(v), _ptr(g), r, c, s) for w, v, g, r, c, s in matrices]
+    return (MuonMatrix * len(rows))(*rows)
+
+
+def muon_workspace_size(mats) -> int:
+    return int(lib().pf16_muon_workspace_size(mats, len(mats)))
+
+
+def muon_update(mats, lr, momentum, wd, ws, flags=PF16_MUON_NESTEROV, steps=5, stream=None):
+    """Momentum, orthogonalised update and decay of every matrix of a muon_list, in place; lr,
+    momentum and wd are floats (sgd_update's are binary16 bits)."""
+    _check(lib().pf16_muon_update(mats, len(mats), lr, momentum, wd, steps, flags, _ptr(ws), _nbytes(ws),
+                                  _stream(stream)), "pf16_muon_update")
+
+
+def quantize_i8(x, q, scale, m, k, stream=None):
+    """Rows of x[m][k] as 8-bit integers q and one float32 scale each."""
+    _check(lib().pf16_quantize_i8(_ptr(x), _ptr(q), _ptr(scale), m, k, _stream(stream)), "pf16_quantize_i8")
+
+
+def linear_i8(x, sx, w, sw, bias, y, m, n, k, stream=None):
+    """y[m][n] = x[m][k] w[n][k]^T in 8-bit integers, scaled by row (sx) and channel (sw), plus bias or None."""
+    _check(lib().pf16_linear_i8(_ptr(x), _ptr(sx), _ptr(w), _ptr(sw), _ptr(bias), _ptr(y), m, n, k, _stream(stream)),
+           "pf16_linear_i8")
 
 
 def sync_status(stream=None) -> int:

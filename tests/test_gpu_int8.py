@@ -1,0 +1,218 @@
+"""8-bit rows and the linear layer over them on the GPU against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+import matrix_oracle as mo
+from paper_1911_07384_gb300 import pf16
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    import torch
+
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def quantize(x, stream=None):
+    import torch
+
+    m, k = x.shape
+    t = dev(x)
+    q = torch.full((m * k + 64,), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((m + 4,), -5.0, dtype=torch.float32, device="cuda")
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    pf16.quantize_i8(t, q, s, m, k, stream=stream)
+    assert pf16.sync_status(stream) == 0
+    assert bool((q[m * k:] == 99).all()) and bool((s[m:] == -5.0).all())
+    return q[:m * k].reshape(m, k).cpu().numpy(), s[:m].cpu().numpy()
+
+
+def check_quantize(x):
+    q, s = quantize(x)
+    want, scale = mo.quantize(x)
+    assert np.array_equal(q, want)
+    assert np.array_equal(s, scale.astype(np.float32), equal_nan=True)  # one division in FP32
+
+
+@pytest.mark.parametrize("m", [1, 3, 33, 1000])
+@pytest.mark.parametrize("k", [1, 2, 7, 8, 31, 64, 72, 128, 147, 256, 1000, 1024, 1032, 2048, 4095])
+def test_quantize(m, k):
+    rng = np.random.default_rng(m * 10007 + k)
+    check_quantize((rng.standard_normal((m, k)) * 2.0 ** rng.integers(-12, 10, (m, 1))).astype(np.float16))
+
+
+@pytest.mark.parametrize("m,k", [(2, 8192), (3, 8200), (2, 30000), (1, 65537), (70001, 8)])
+def test_quantize_long_and_many_rows(m, k):
+    rng = np.random.default_rng(k)
+    check_quantize(rng.standard_normal((m, k)).astype(np.float16))
+
+
+@pytest.mark.parametrize("k", [40, 41, 1500])
+def test_quantize_edge_rows(k):
+    """Zero rows, rows with infinities and NaNs, single values, subnormals, ties, the largest number."""
+    rng = np.random.default_rng(k)
+    x = np.zeros((12, k), np.float16)
+    x[1, k - 1] = np.inf
+    x[2] = rng.standard_normal(k)
+    x[2, k // 2] = np.nan
+    x[3] = -np.inf
+    x[4, 0] = -6e-8
+    x[5] = np.arange(k) % 9 * np.float16(6e-8)
+    x[6] = 65504
+    x[7] = np.where(np.arange(k) % 2, 1.0, 0.5)      # 63.5 is a tie, to 64
+    x[8] = np.where(np.arange(k) % 2, -254.0, 5.0)   # 2.5 is a tie, to 2
+    x[9] = np.where(np.arange(k) % 2, 254.0, -3.0)   # -1.5 is a tie, to -2
+    x[10, 1:] = -0.0
+    x[11] = rng.standard_normal(k) * 1e-6
+    check_quantize(x)
+    q, s = quantize(x)
+    assert not q[[0, 1, 2, 3, 10]].any() and np.isnan(s[[1, 2, 3]]).all() and s[0] == 0
+    assert q[7, 0] == 64 and q[8, 0] == 2 and q[9, 0] == -2
+
+
+def test_quantize_every_quotient():
+    """Every |x| <= a for several a: all ties and near ties that two binary16 numbers can make."""
+    for a in (0x3C00, 0x3C01, 0x3FFF, 0x0400, 0x03FF, 0x7BFF, 0x57F0):
+        x = np.arange(a + 1, dtype=np.uint16).view(np.float16)
+        check_quantize(np.stack([x, -x]))
+
+
+def linear(x, sx, w, sw, bias, stream=None):
+    import torch
+
+    m, n = len(x), len(w)
+    y = torch.full((m * n + 64,), -7.0, dtype=torch.float16, device="cuda")
+    ts = [dev(a) for a in (x, sx, w, sw)]
+    tb = None if bias is None else dev(bias)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    pf16.linear_i8(*ts, tb, y, m, n, x.shape[1], stream=stream)
+    assert pf16.sync_status(stream) == 0
+    assert bool((y[m * n:] == -7.0).all())
+    return y[:m * n].reshape(m, n).cpu().numpy()
+
+
+def operands(rng, m, n, k, extreme=False):
+    if extreme:  # the largest products, all of one sign in some places: -128 and 127
+        x = np.where(rng.random((m, k)) < 0.9, -128, 127).astype(np.int8)
+        w = np.where(rng.random((n, k)) < 0.9, -128, 127).astype(np.int8)
+    else:
+        x, w = (rng.integers(-128, 128, s).astype(np.int8) for s in ((m, k), (n, k)))
+    sx, sw = ((rng.random(s) + 0.1).astype(np.float32) * 1e-2 for s in (m, n))
+    return x, sx, w, sw, rng.standard_normal(n).astype(np.float16)
+
+
+def check_linear(x, sx, w, sw, bias, y):
+    want, slack = mo.linear(x, sx, w, sw, bias)
+    tol = slack + mo.U16 * (np.abs(want) + slack) + mo.TINY16
+    big = np.abs(want) > 65519  # rounds to infinity
+    assert np.array_equal(np.isinf(y), big)
+    err = np.abs(np.where(big, 0, y.astype(np.float64)) - np.where(big, 0, want))
+    assert np.all(err <= tol), (err / tol).max()
+
+
+LINEAR = [(1, 1, 1), (1, 8, 16), (1, 1000, 2048), (2, 100, 64), (3, 5, 33), (4, 129, 128), (5, 64, 100), (7, 300, 15),
+          (8, 1000, 512), (9, 257, 160), (16, 512, 1040), (17, 65, 65), (31, 1001, 77), (33, 128, 2048), (64, 64, 64),
+          (65, 200, 192), (100, 1000, 2048), (127, 127, 127), (128, 256, 512), (129, 255, 144), (256, 1000, 2048),
+          (300, 520, 1088), (1000, 64, 256), (640, 384, 48), (513, 1024, 320), (2, 8192, 96), (40, 3000, 4608)]
+
+
+@pytest.mark.parametrize("m,n,k", LINEAR)
+def test_linear(m, n, k):
+    rng = np.random.default_rng(m * 31 + n * 17 + k)
+    for bias in (True, False):
+        x, sx, w, sw, b = operands(rng, m, n, k)
+        b = b if bias else None
+        check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 64, 1024), (6, 130, 1024), (130, 70, 1024), (20, 260, 1024), (300, 300, 1024)])
+def test_linear_sums_are_exact(m, n, k):
+    """Scales of one: sums up to 1024 * 128^2 = 2^24 come out as binary16 rounds the exact integers
+    (scaled so that none overflows)."""
+    rng = np.random.default_rng(k + m)
+    x, _, w, _, _ = operands(rng, m, n, k, extreme=True)
+    x[0], w[0] = -128, -128  # 2^24 itself
+    sx, sw = np.full(m, 2.0 ** -6, np.float32), np.full(n, 2.0 ** -5, np.float32)
+    want = (x.astype(np.int64) @ w.astype(np.int64).T).astype(np.float64) * 2.0 ** -11
+    assert np.array_equal(linear(x, sx, w, sw, None), want.astype(np.float16))
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 4608), (50, 300, 5000), (200, 200, 8192), (1, 9, 65536), (70, 9, 65536)])
+def test_linear_long_sums(m, n, k):
+    rng = np.random.default_rng(k)
+    x, sx, w, sw, b = operands(rng, m, n, k, extreme=True)
+    sx *= np.float32(2.0 ** -8)
+    check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
+
+
+@pytest.mark.parametrize("m", [2, 40, 200])
+def test_linear_scales_that_are_not_finite(m):
+    """A NaN scale makes its row or channel NaN, and no other; zero scales give the bias."""
+    rng = np.random.default_rng(m)
+    x, sx, w, sw, b = operands(rng, m, 90, 96)
+    sx[1], sw[7], sw[8] = np.nan, np.nan, 0
+    y = linear(x, sx, w, sw, b)
+    nan = np.zeros((m, 90), bool)
+    nan[1], nan[:, 7] = True, True
+    assert np.array_equal(np.isnan(y), nan)
+    assert np.array_equal(y[0, 8], b[8])
+
+
+def test_linear_same_bits_and_other_stream():
+    import torch
+
+    for m, n, k in ((3, 500, 1000), (48, 1000, 2048), (300, 260, 2048)):
+        x, sx, w, sw, b = operands(np.random.default_rng(m), m, n, k)
+        one = linear(x, sx, w, sw, b)
+        assert np.array_equal(one, linear(x, sx, w, sw, b, stream=torch.cuda.Stream()))
+        # a row's result does not depend on the rows around it as far as sums are exact
+        assert np.array_equal(one, linear(x, sx, w, sw, b))
+
+
+def test_rows_quantised_and_multiplied():
+    """The two together, as a classifier uses them: against the product of the binary16 rows, off by
+    at most half a step of each integer (s/2 a term) and the roundings."""
+    m, n, k = 70, 1000, 2048
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((m, k)).astype(np.float16)
+    w = (rng.standard_normal((n, k)) * 0.03).astype(np.float16)
+    (xq, sx), (wq, sw) = quantize(x), quantize(w)
+    y = linear(xq, sx, wq, sw, None).astype(np.float64)
+    x64, w64 = x.astype(np.float64), w.astype(np.float64)
+    half_x, half_w = sx.astype(np.float64)[:, None] / 2, sw.astype(np.float64)[:, None] / 2
+    bound = half_x * np.abs(w64).sum(1)[None, :] + np.abs(x64).sum(1)[:, None] * half_w.T + k * half_x * half_w.T
+    want = x64 @ w64.T
+    assert np.all(np.abs(y - want) <= bound * (1 + 2.0 ** -10) + 2 * mo.U16 * np.abs(want))
+
+
+def test_captured_and_replayed():
+    import torch
+
+    rng = np.random.default_rng(12)
+    m, n, k = 24, 200, 256
+    xs = [rng.standard_normal((m, k)).astype(np.float16) for _ in range(3)]
+    _, _, w, sw, b = operands(rng, m, n, k)
+    x, q, s = dev(xs[0]), torch.zeros(m, k, dtype=torch.int8, device="cuda"), torch.zeros(m, device="cuda")
+    tw, tsw, tb, y = dev(w), dev(sw), dev(b), torch.zeros(m, n, dtype=torch.float16, device="cuda")
+
+    def both():
+        pf16.quantize_i8(x, q, s, m, k)
+        pf16.linear_i8(q, s, tw, tsw, tb, y, m, n, k)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        both()
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            both()
+        for a in xs:
+            x.copy_(dev(a))
+            graph.replay()
+            assert pf16.sync_status(st) == 0
+            qq, ss = mo.quantize(a)
+            check_linear(qq, ss.astype(np.float32), w, sw, b, y.cpu().numpy())

@@ -1,0 +1,221 @@
+"""Orthogonalised updates on the GPU against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+import matrix_oracle as mo
+from paper_1911_07384_gb300 import pf16
+
+pytestmark = pytest.mark.gpu
+
+
+def gradient(rng, rows, cols, kind="noise"):
+    g = rng.standard_normal((rows, cols))
+    if kind == "lowrank":  # a few directions over 1% of noise
+        r = max(1, min(rows, cols) // 16)
+        g = rng.standard_normal((rows, r)) @ rng.standard_normal((r, cols)) + 0.01 * g
+    return (g * 0.02).astype(np.float16)
+
+
+def dev(a):
+    import torch
+
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def space(nbytes):
+    import torch
+
+    return torch.full((nbytes,), 0xFF, dtype=torch.uint8, device="cuda")  # NaNs, whatever the type
+
+
+def ortho(gs, steps=5, ws=None, stream=None):
+    """Results of one call, as float64 arrays, with the elements behind each output checked."""
+    import torch
+
+    ins = [dev(g) for g in gs]
+    outs = [torch.full((g.size + 64,), -7.0, dtype=torch.float16, device="cuda") for g in gs]
+    mats = pf16.ortho_list([(i, o, *g.shape) for i, o, g in zip(ins, outs, gs)])
+    need = pf16.ortho_workspace_size(mats)
+    ws = space(need) if ws is None else ws
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    pf16.orthogonalize(mats, ws, steps=steps, stream=stream)
+    assert pf16.sync_status(stream) == 0
+    for o, i, g in zip(outs, ins, gs):
+        assert bool((o[g.size:] == -7.0).all())
+        assert np.array_equal(i.cpu().numpy().view(np.uint16), g.view(np.uint16))
+    return [o[:g.size].reshape(g.shape).cpu().numpy().astype(np.float64) for o, g in zip(outs, gs)]
+
+
+def check(got, g, steps=5):
+    want = mo.orthogonal(g, steps)
+    tol = mo.orthogonal_tolerance(g, steps) + mo.U16 * np.linalg.norm(want) + mo.TINY16 * np.sqrt(g.size)
+    assert np.isfinite(got).all()
+    assert np.linalg.norm(got - want) <= tol, (g.shape, np.linalg.norm(got - want), tol)
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (8, 8), (63, 65), (64, 64), (65, 64), (64, 147), (147, 64), (128, 128),
+          (129, 127), (130, 250), (200, 129), (256, 64), (64, 576), (192, 320), (321, 193), (500, 333), (1, 4097),
+          (3000, 2)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_shapes(rows, cols):
+    g = gradient(np.random.default_rng(rows * 7919 + cols), rows, cols)
+    check(ortho([g])[0], g)
+
+
+@pytest.mark.parametrize("rows,cols", [(96, 96), (128, 512), (400, 256), (1000, 2048)])
+@pytest.mark.parametrize("kind", ["noise", "lowrank"])
+def test_spectra(rows, cols, kind):
+    g = gradient(np.random.default_rng(5), rows, cols, kind)
+    check(ortho([g])[0], g)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 7])
+def test_steps(steps):
+    g = gradient(np.random.default_rng(steps), 100, 140)
+    check(ortho([g], steps)[0], g, steps)
+
+
+def test_many_matrices_in_one_call():
+    rng = np.random.default_rng(11)
+    gs = [gradient(rng, *s) for s in SHAPES] + [gradient(rng, int(r), int(c))
+                                               for r, c in rng.integers(1, 200, (235, 2))]
+    assert len(gs) == 256
+    got = ortho(gs)
+    for o, g in zip(got, gs):
+        check(o, g)
+    # a matrix's result does not depend on the others of its call
+    for i in (0, 13, 20, 100):
+        assert np.array_equal(ortho([gs[i]])[0], got[i])
+
+
+def test_values_at_the_edges():
+    rng = np.random.default_rng(2)
+    g = gradient(rng, 70, 90)
+    zero = np.zeros((70, 90), np.float16)
+    one = zero.copy()
+    one[3, 5] = -6e-8  # a single subnormal element: singular value one
+    bad = [g.copy() for _ in range(3)]
+    bad[0][1, 2], bad[1][69, 89], bad[2][0, 0] = np.inf, np.nan, -np.inf
+    big = np.full((70, 90), 65504, np.float16)
+    got = ortho([g, zero, one, big, *bad])
+    check(got[0], g)
+    assert not got[1].any()
+    check(got[2], one)
+    assert np.count_nonzero(got[2]) == 1
+    check(got[3], big)
+    for o in got[4:]:
+        assert np.isnan(o).all()
+    # a power of two in the input changes nothing at all
+    assert np.array_equal(ortho([(g.astype(np.float32) * 64).astype(np.float16)])[0], got[0])
+
+
+def test_same_bits_again_in_place_and_on_another_stream():
+    import torch
+
+    rng = np.random.default_rng(4)
+    gs = [gradient(rng, 300, 700), gradient(rng, 257, 64)]
+    first = ortho(gs)
+    again = ortho(gs, stream=torch.cuda.Stream())
+    ts = [dev(g) for g in gs]
+    mats = pf16.ortho_list([(t, t, *g.shape) for t, g in zip(ts, gs)])
+    pf16.orthogonalize(mats, space(pf16.ortho_workspace_size(mats)))
+    assert pf16.sync_status() == 0
+    for a, b, t in zip(first, again, ts):
+        assert np.array_equal(a, b)
+        assert np.array_equal(a, t.cpu().numpy().astype(np.float64))
+
+
+def test_captured_and_replayed_with_a_shared_workspace():
+    import torch
+
+    rng = np.random.default_rng(6)
+    gs = [gradient(rng, 96, 200), gradient(rng, 210, 130)]
+    ts, outs = [dev(g) for g in gs], [torch.zeros(g.shape, dtype=torch.float16, device="cuda") for g in gs]
+    lists = [pf16.ortho_list([(t, o, *g.shape)]) for t, o, g in zip(ts, outs, gs)]
+    ws = space(max(pf16.ortho_workspace_size(m) for m in lists))
+    s = torch.cuda.Stream()
+    graphs = []
+    with torch.cuda.stream(s):
+        pf16.orthogonalize(lists[0], ws)  # (set up before the capture)
+        s.synchronize()
+        for m in lists:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                pf16.orthogonalize(m, ws)
+            graphs.append(graph)
+        for _ in range(3):
+            for t, g in zip(ts, gs):
+                t.copy_(dev(g * np.float16(0.5)))  # new contents of the same buffers
+            for o in outs:
+                o.zero_()
+            for graph in graphs:
+                graph.replay()
+    assert pf16.sync_status(s) == 0
+    for o, g in zip(outs, gs):
+        check(o.cpu().numpy().astype(np.float64), g * np.float16(0.5))
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: neither call needs the whole GPU to end."""
+    import torch
+
+    rng = np.random.default_rng(8)
+    gs = [gradient(rng, 700, 900), gradient(rng, 900, 700)]
+    alone = [ortho([g])[0] for g in gs]
+    ts, outs = [dev(g) for g in gs], [torch.zeros(g.shape, dtype=torch.float16, device="cuda") for g in gs]
+    lists = [pf16.ortho_list([(t, o, *g.shape)]) for t, o, g in zip(ts, outs, gs)]
+    wss = [space(pf16.ortho_workspace_size(m)) for m in lists]
+    streams = [torch.cuda.Stream() for _ in gs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for m, ws, s in zip(lists, wss, streams):
+            pf16.orthogonalize(m, ws, stream=s)
+    assert [pf16.sync_status(s) for s in streams] == [0, 0]
+    for o, a in zip(outs, alone):
+        assert np.array_equal(o.cpu().numpy().astype(np.float64), a)
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (64, 147), (65, 64), (300, 130), (128, 1152)])
+def test_muon(rows, cols, nesterov):
+    rng = np.random.default_rng(rows + cols)
+    w, v, g = ((rng.standard_normal((rows, cols)) * s).astype(np.float16) for s in (0.1, 0.05, 0.02))
+    lr, momentum, wd, scale = 0.02, 0.95, 0.1, float(np.sqrt(max(1, rows / cols)))
+    tw, tv, tg = dev(w), dev(v), dev(g)
+    mats = pf16.muon_list([(tw, tv, tg, rows, cols, scale)])
+    ws = space(pf16.muon_workspace_size(mats))
+    for _ in range(2):  # the second step starts from what the first has stored
+        w64, v64, u = mo.muon(w, v, g, lr, momentum, wd, scale, nesterov)
+        pf16.muon_update(mats, lr, momentum, wd, ws, flags=pf16.PF16_MUON_NESTEROV if nesterov else 0)
+        assert pf16.sync_status() == 0
+        w, v = tw.cpu().numpy(), tv.cpu().numpy()
+        # one FMA in FP32 and one rounding to binary16
+        assert np.all(np.abs(v - v64) <= (mo.U16 + 2.0 ** -23) * np.abs(v64) + mo.TINY16)
+        # the update's error, and one rounding of the weight
+        tol = lr * scale * mo.orthogonal_tolerance(u) + (mo.U16 + 2.0 ** -21) * np.linalg.norm(w64)
+        tol += mo.TINY16 * np.sqrt(w.size)
+        assert np.linalg.norm(w - w64) <= tol
+        assert np.array_equal(tg.cpu().numpy(), g)
+
+
+def test_muon_of_a_poisoned_gradient_leaves_the_other_matrices():
+    rng = np.random.default_rng(9)
+    ws_, vs, gs = ([(rng.standard_normal((48, 80)) * 0.1).astype(np.float16) for _ in range(2)] for _ in range(3))
+    gs[0][5, 6] = np.inf
+    tw, tv, tg = ([dev(a) for a in x] for x in (ws_, vs, gs))
+    mats = pf16.muon_list([(w, v, g, 48, 80, 1.0) for w, v, g in zip(tw, tv, tg)])
+    pf16.muon_update(mats, 0.1, 0.9, 0.0, space(pf16.muon_workspace_size(mats)))
+    assert pf16.sync_status() == 0
+    assert bool(tw[0].isnan().all()) and bool(tw[1].isfinite().all())
+    # momentum zero and gradient zero: the weights only decay
+    z = dev(np.zeros((48, 80), np.float16))
+    w0 = ws_[1]
+    tw1, tv1 = dev(w0), z.clone()
+    mats = pf16.muon_list([(tw1, tv1, z, 48, 80, 1.0)])
+    pf16.muon_update(mats, 0.5, 0.9, 0.5, space(pf16.muon_workspace_size(mats)))
+    assert pf16.sync_status() == 0
+    assert np.array_equal(tw1.cpu().numpy(), (w0.astype(np.float32) * np.float32(0.75)).astype(np.float16))
+    assert not bool(tv1.any())

@@ -1,0 +1,163 @@
+"""Refusals of the orthogonalised update and of the 8-bit linear layer: every invalid call
+returns its documented status on the host, before anything is launched."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_1911_07384_gb300 import pf16
+
+MIB = 1 << 20
+
+
+class T:
+    """What the binding asks of a tensor: an address (never dereferenced) and a size."""
+
+    def __init__(self, at, nbytes=0):
+        self.at, self.nbytes = at, nbytes
+
+    def data_ptr(self):
+        return self.at
+
+
+G, O, V, WS = (T(i * 64 * MIB) for i in range(1, 5))
+
+
+def refused(code, fn, *args, **kw):
+    with pytest.raises(pf16.PF16Error) as e:
+        fn(*args, stream=0, **kw)
+    assert e.value.code == code, (e.value.code, code)
+
+
+def ortho(code, rows=8, cols=8, g=G, o=O, ws=WS, ws_bytes=None, **kw):
+    mats = pf16.ortho_list([(g, o, rows, cols)])
+    need = pf16.ortho_workspace_size(mats)
+    ws = T(ws.at, need if ws_bytes is None else ws_bytes) if ws is not None else None
+    refused(code, pf16.orthogonalize, mats, ws, **kw)
+
+
+def test_orthogonalize_refusals():
+    for rows, cols in ((0, 8), (8, 0), (-1, 8), (65537, 1), (32769, 32769)):
+        assert pf16.ortho_workspace_size(pf16.ortho_list([(G, O, rows, cols)])) == 0
+        ortho(pf16.PF16_ERR_SHAPE, rows, cols)
+    for steps in (0, -1, 17):
+        ortho(pf16.PF16_ERR_ARG, steps=steps)
+    ortho(pf16.PF16_ERR_NULL, g=None)
+    ortho(pf16.PF16_ERR_NULL, o=None)
+    ortho(pf16.PF16_ERR_ALIGN, g=T(G.at + 2))
+    ortho(pf16.PF16_ERR_ALIGN, o=T(O.at + 8))
+    ortho(pf16.PF16_ERR_ALIGN, ws=T(WS.at + 8))
+    ortho(pf16.PF16_ERR_WORKSPACE, ws=None)
+    need = pf16.ortho_workspace_size(pf16.ortho_list([(G, O, 8, 8)]))
+    assert need > 0
+    ortho(pf16.PF16_ERR_WORKSPACE, ws_bytes=need - 1)
+    # an output meets its own input only as a whole, and nothing else
+    ortho(pf16.PF16_ERR_ARG, o=T(G.at + 16))
+    ortho(pf16.PF16_ERR_ARG, o=T(WS.at + 64))
+    ortho(pf16.PF16_ERR_ARG, g=T(WS.at + 64))
+    two = pf16.ortho_list([(G, O, 8, 8), (V, T(O.at + 112), 8, 8)])
+    refused(pf16.PF16_ERR_ARG, pf16.orthogonalize, two, T(WS.at, pf16.ortho_workspace_size(two)))
+    two = pf16.ortho_list([(G, O, 8, 8), (O, V, 8, 8)])  # one's output is another's input
+    refused(pf16.PF16_ERR_ARG, pf16.orthogonalize, two, T(WS.at, pf16.ortho_workspace_size(two)))
+
+
+def test_list_lengths():
+    many = pf16.ortho_list([(T(G.at + 256 * i), T(O.at + 256 * i), 4, 4) for i in range(257)])
+    assert pf16.ortho_workspace_size(many) == 0
+    refused(pf16.PF16_ERR_UNSUPPORTED, pf16.orthogonalize, many, T(WS.at, MIB))
+    full = (pf16.OrthoMatrix * 256).from_buffer(many)
+    assert pf16.ortho_workspace_size(full) > 0
+    pf16.orthogonalize(pf16.ortho_list([]), None, stream=0)  # nothing to do
+    pf16.muon_update(pf16.muon_list([]), 0.1, 0.9, 0.0, None, stream=0)
+    L = pf16.lib()
+    assert L.pf16_orthogonalize(None, 1, 5, None, 0, None) == pf16.PF16_ERR_NULL
+    assert L.pf16_muon_update(None, 1, 0.1, 0.9, 0.0, 5, 0, None, 0, None) == pf16.PF16_ERR_NULL
+    assert L.pf16_orthogonalize(None, -1, 5, None, 0, None) == pf16.PF16_ERR_SHAPE
+    assert L.pf16_muon_workspace_size(None, 3) == 0
+
+
+def test_muon_refusals():
+    def muon(code, w=O, v=V, g=G, scale=1.0, lr=0.1, momentum=0.9, wd=0.0, **kw):
+        mats = pf16.muon_list([(w, v, g, 8, 8, scale)])
+        refused(code, pf16.muon_update, mats, lr, momentum, wd, T(WS.at, pf16.muon_workspace_size(mats)), **kw)
+
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        for name in ("scale", "lr", "momentum", "wd"):
+            muon(pf16.PF16_ERR_ARG, **{name: bad})
+    muon(pf16.PF16_ERR_ARG, flags=2)
+    muon(pf16.PF16_ERR_ARG, steps=0)
+    for name in ("w", "v", "g"):
+        muon(pf16.PF16_ERR_NULL, **{name: None})
+        muon(pf16.PF16_ERR_ALIGN, **{name: T(8 * 64 * MIB + 2)})
+    muon(pf16.PF16_ERR_ARG, w=G)
+    muon(pf16.PF16_ERR_ARG, v=G)
+    muon(pf16.PF16_ERR_ARG, w=V)
+
+
+def test_workspace_covers_the_padded_matrices():
+    """X twice in binary16 and once in FP32, S and the quintic's factor, in blocks of 64 x 64."""
+    for rows, cols in ((1, 1), (64, 64), (65, 64), (1000, 2048), (2048, 1000), (512, 4608)):
+        m, n = (-(-s // 64) * 64 for s in sorted((rows, cols)))
+        need = pf16.ortho_workspace_size(pf16.ortho_list([(G, O, rows, cols)]))
+        assert 0 <= need - (8 * m * n + 4 * m * m) <= 4096
+        assert need == pf16.muon_workspace_size(pf16.muon_list([(O, V, G, rows, cols, 1.0)]))
+
+
+def test_quantize_refusals():
+    Q, S = O, V
+
+    def quant(code, x=G, q=Q, s=S, m=4, k=8):
+        refused(code, pf16.quantize_i8, x, q, s, m, k)
+
+    quant(pf16.PF16_ERR_SHAPE, m=-1)
+    quant(pf16.PF16_ERR_SHAPE, k=0)
+    for name in "xqs":
+        quant(pf16.PF16_ERR_NULL, **{name: None})
+        quant(pf16.PF16_ERR_ALIGN, **{name: T(512 * MIB + 2)})
+    quant(pf16.PF16_ERR_ARG, q=G)
+    quant(pf16.PF16_ERR_ARG, s=T(G.at + 60))
+    quant(pf16.PF16_ERR_ARG, s=T(Q.at + 28))
+    pf16.quantize_i8(None, None, None, 0, 8, stream=0)  # no rows
+
+
+def test_linear_refusals():
+    x, sx, w, sw, bias, y = (T(i * 64 * MIB) for i in range(1, 7))
+
+    def linear(code, m=4, n=4, k=32, **kw):
+        a = dict(x=x, sx=sx, w=w, sw=sw, bias=bias, y=y) | kw
+        refused(code, pf16.linear_i8, a["x"], a["sx"], a["w"], a["sw"], a["bias"], a["y"], m, n, k)
+
+    for size in (dict(m=-1), dict(n=0), dict(k=0), dict(k=65537)):
+        linear(pf16.PF16_ERR_SHAPE, **size)
+    for name in ("x", "sx", "w", "sw", "y"):
+        linear(pf16.PF16_ERR_NULL, **{name: None})
+        linear(pf16.PF16_ERR_ALIGN, **{name: T(512 * MIB + 2)})
+    linear(pf16.PF16_ERR_ALIGN, bias=T(bias.at + 1))
+    for name in ("x", "w"):
+        linear(pf16.PF16_ERR_ARG, **{name: T(y.at - 112)})
+    linear(pf16.PF16_ERR_ARG, sx=T(y.at + 4))
+    linear(pf16.PF16_ERR_ARG, bias=T(y.at))
+    pf16.linear_i8(x, sx, w, sw, None, y, 0, 4, 32, stream=0)  # no rows
+
+
+def test_quotients_of_binary16_numbers_stay_off_ties():
+    """What the quantiser's rounding rests on: 127 x / a in FP32 rounds to the integer that the
+    real quotient rounds to, for every |x| <= a of random a (ties, which are exact, among them)."""
+    rng = np.random.default_rng(3)
+    for bits in np.concatenate([rng.integers(1, 0x7C00, 60), [1, 2, 0x3FF, 0x400, 0x7BFF, 0x3C00]]):
+        a = np.uint16(bits).view(np.float16)
+        x = np.arange(int(bits) + 1, dtype=np.uint16).view(np.float16)
+        q32 = (x.astype(np.float32) * np.float32(127)) / np.float32(a)
+        # the real quotient's rounding from integers: x = i 2^e, a = j 2^f
+        mi, ei = np.frexp(x.astype(np.float64))
+        ma, ea = np.frexp(np.float64(a))
+        num = (mi * 2 ** 11).astype(np.int64) * 127 * 2
+        den = np.int64(ma * 2 ** 11)
+        shift = (ea - ei).astype(np.int64)
+        small = shift > 40  # the quotient is far below one half
+        den = den << np.clip(shift, 0, 40)  # (x = 0 has no exponent)
+        whole = (num // den + 1) // 2                      # round half up of num / (2 den)
+        tie = (num % den == 0) & ((num // den) % 2 == 1)
+        whole = np.where(tie & (whole % 2 == 1), whole - 1, whole)
+        whole = np.where(small, 0, whole)
+        assert np.array_equal(np.rint(q32).astype(np.int64), whole), a
