@@ -153,6 +153,16 @@ namespace {
 template <bool ALIGNED>
 __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
   if (ALIGNED) return c < k ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+  // Whole words around the 16 bytes while they end inside the row (they start in the
+  // array: rows before this one, or the array's aligned start, precede it).
+  const int lead = (int)(reinterpret_cast<uintptr_t>(row + c) & 3u);
+  if (c + 16 + ((4 - lead) & 3) <= k) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(row + c - lead);
+    const uint32_t w0 = __ldg(w), w1 = __ldg(w + 1), w2 = __ldg(w + 2), w3 = __ldg(w + 3);
+    const uint32_t w4 = lead ? __ldg(w + 4) : 0u;
+    return make_uint4(__funnelshift_r(w0, w1, lead * 8), __funnelshift_r(w1, w2, lead * 8),
+                      __funnelshift_r(w2, w3, lead * 8), __funnelshift_r(w3, w4, lead * 8));
+  }
   uint32_t v[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < 16; ++j)
@@ -196,14 +206,339 @@ __global__ void __launch_bounds__(256) k_linear_i8_rows(const LinearI8 a) {
   }
 }
 
-cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s) {
-  (void)sms;
-  (void)status;
-  const bool al = (a.k & 15) == 0;
-  const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)((a.m + 7) / 8));
-  const cudaError_t e = al ? launch_pdl(k_linear_i8_rows<8, true>, grid, dim3(256), 0, s, a)
-                           : launch_pdl(k_linear_i8_rows<8, false>, grid, dim3(256), 0, s, a);
+// ---------------------------------------------------------------------------
+// The product on the tensor cores.
+//
+// sm_103a's tcgen05.mma has no 8-bit integer kind.  An 8-bit integer is exact
+// in binary16, a product of two in FP32, and so is a sum of 1024 of them, so
+// the integers are multiplied as binary16 at the 16-bit rate.  The conversion
+// sits between global memory and the swizzled operand tiles: eight warps load
+// 16 bytes a lane (half the bytes that binary16 operands would move), widen
+// them by byte permutes -- 0x6400 | (x + 128) is 1152 + x in binary16, and a
+// subtraction gives x -- and store them where tcgen05.mma reads them.
+//
+// D[p][q] = sum_k P[p][k] Q[q][k]: 128 rows of P against BN of Q.  P is x and
+// Q is w, or, with few rows of x (SWAP), P is w and Q is x, so that the 128
+// rows of an MMA are always filled.  A cluster of CTAs can share a tile's K:
+// each sums its part and the parts are added in rank order through
+// distributed shared memory.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kI8Threads = 288;  // eight converting (then storing) warps, one MMA warp
+
+template <int BN>
+struct I8Cfg {
+  static constexpr int STAGE = (128 + BN) * 128;
+  static constexpr int STAGES = BN >= 256 ? 4 : BN >= 128 ? 3 : 4;
+  static constexpr int DIST = BN >= 128 ? 2 : 4;  // K-blocks of raw bytes in registers ahead of the conversion
+  static constexpr int CTAS = BN >= 256 ? 1 : 2;
+  static constexpr int SMEM = 1024 + STAGES * STAGE;
+  static constexpr int TMEM = BN < 32 ? 32 : BN;
+  static constexpr int UQ = (BN * 4 + 255) / 256;  // 16-byte units of Q a thread loads per K-block
+  static constexpr int U = 2 + UQ;
+};
+
+// 4 int8 -> 4 binary16
+__device__ __forceinline__ uint2 widen4(uint32_t v) {
+  v ^= 0x80808080u;
+  return make_uint2(hsub2_rn(prmt(v, 0x64646464u, 0x4140u), 0x64806480u),
+                    hsub2_rn(prmt(v, 0x64646464u, 0x4342u), 0x64806480u));
+}
+// 16 int8 as 32 bytes of a tile's row: chunks 2 c and 2 c + 1 of its eight
+__device__ __forceinline__ void put16(uint32_t tile, int row, int c, const uint4& v) {
+  const uint2 a = widen4(v.x), b = widen4(v.y), d = widen4(v.z), e = widen4(v.w);
+  const uint32_t at = tile + (uint32_t)row * 128u;
+  st_shared_v4(at + (uint32_t)(((2 * c) ^ (row & 7)) << 4), make_uint4(a.x, a.y, b.x, b.y));
+  st_shared_v4(at + (uint32_t)(((2 * c + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t saddr, uint32_t rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// y for `cnt` consecutive columns q0.. of row p
+template <bool SWAP>
+__device__ __forceinline__ void store_y(const LinearI8& a, int p, int q0, const float* acc, int cnt) {
+  if (SWAP) {  // p is a channel, the columns are rows of x: neighbouring lanes write neighbouring channels
+    if (p >= a.n) return;
+    const float sw = a.sw[p], b = a.bias ? h2f(a.bias[p]) : 0.f;
+    for (int j = 0; j < cnt; ++j)
+      if (q0 + j < a.m) a.y[(long long)(q0 + j) * a.n + p] = f2h(fmaf(acc[j], a.sx[q0 + j] * sw, b));
+  } else {
+    if (p >= a.m) return;
+    const float sx = a.sx[p];
+    uint16_t* o = a.y + (long long)p * a.n + q0;
+    if ((a.n & 7) == 0) {
+      for (int h = 0; h + 8 <= cnt; h += 8) {
+        if (q0 + h >= a.n) return;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          v[j] = fmaf(acc[h + j], sx * __ldg(a.sw + q0 + h + j), a.bias ? h2f(__ldg(a.bias + q0 + h + j)) : 0.f);
+        *reinterpret_cast<uint4*>(o + h) =
+            make_uint4(f2h2(v[0], v[1]), f2h2(v[2], v[3]), f2h2(v[4], v[5]), f2h2(v[6], v[7]));
+      }
+    } else {
+      for (int j = 0; j < cnt; ++j)
+        if (q0 + j < a.n)
+          o[j] = f2h(fmaf(acc[j], sx * __ldg(a.sw + q0 + j), a.bias ? h2f(__ldg(a.bias + q0 + j)) : 0.f));
+    }
+  }
+}
+
+}  // namespace
+
+template <int BN, bool SWAP, bool ALIGNED>
+__global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
+    k_linear_i8_mma(const LinearI8 a, int q_tiles, int splits, int* status, unsigned long long lim) {
+  using Cfg = I8Cfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  __shared__ uint64_t full[Cfg::STAGES], empty[Cfg::STAGES], done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int drained;
+  const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < Cfg::STAGES; ++i) {
+      mbar_init(smem_u32(&full[i]), 8);
+      mbar_init(smem_u32(&empty[i]), 1);
+    }
+    mbar_init(smem_u32(&done), 1);
+    drained = 1;
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(smem_u32(&tmem_slot), Cfg::TMEM);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = tmem_slot;
+  const int rank = splits > 1 ? (int)cluster_rank() : 0;
+  const int tile = (int)blockIdx.x / splits;
+  const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
+  const int kbs = (a.k + 63) >> 6, per = (kbs + splits - 1) / splits;
+  const int kb0 = rank * per, kb1 = kb0 + per < kbs ? kb0 + per : kbs;  // (a rank may be left without any)
+  const int nk = kb1 > kb0 ? kb1 - kb0 : 0;
+  const int P = SWAP ? a.n : a.m, Q = SWAP ? a.m : a.n;
+
+  if (warp == 8) {
+    if (elect_one()) {
+      const uint64_t desc = smem_desc(0, 16, 1024, 2);
+      const uint32_t idesc = idesc_f16(128, BN, false, false, true);
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int i = 0; i < nk; ++i) {
+        if (!mbar_wait(smem_u32(&full[stage]), phase, lim)) {
+          atomicCAS(status, 0, -7);  // PF16_ERR_TIMEOUT
+          break;
+        }
+        tc_fence_after();
+        const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE));
+        const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          tc_mma_f16(tmem, ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc, i > 0 || kk > 0);
+        tc_commit(smem_u32(&empty[stage]));
+        if (++stage == Cfg::STAGES) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+      tc_commit(smem_u32(&done));
+      if (!mbar_wait(smem_u32(&done), 0, lim)) drained = 0;
+    }
+    __syncwarp();
+  } else {
+    // unit u of a K-block: bytes 16 (u & 3) of row u >> 2; P's 512 units first, then Q's
+    const int8_t* base[Cfg::U];
+    bool live[Cfg::U];
+    const int c = tid & 3;
+#pragma unroll
+    for (int i = 0; i < Cfg::U; ++i) {
+      const int r = (tid >> 2) + (i < 2 ? i : i - 2) * 64;
+      const bool in_p = i < 2;
+      const int row = (in_p ? p0 : q0) + r;
+      live[i] = in_p ? row < P : (r < BN && row < Q);
+      const int8_t* from = in_p == SWAP ? a.w : a.x;
+      base[i] = from + (long long)(live[i] ? row : 0) * a.k;
+    }
+    uint4 raw[Cfg::DIST][Cfg::U];
+    auto fetch = [&](int i, uint4* dst) {
+      const int at = (kb0 + i) * 64 + c * 16;
+#pragma unroll
+      for (int u = 0; u < Cfg::U; ++u)
+        dst[u] = live[u] && i < nk ? load16<ALIGNED>(base[u], at, a.k) : make_uint4(0, 0, 0, 0);
+    };
+#pragma unroll
+    for (int d = 0; d < Cfg::DIST; ++d) fetch(d, raw[d]);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int i = 0; ok && i < nk; i += Cfg::DIST) {
+#pragma unroll
+      for (int d = 0; d < Cfg::DIST; ++d) {
+        if (!ok || i + d >= nk) break;
+        ok = mbar_wait(smem_u32(&empty[stage]), phase ^ 1, lim);
+        if (!ok) {
+          atomicCAS(status, 0, -7);
+          break;
+        }
+        const uint32_t sp = smem_u32(smem + stage * Cfg::STAGE), sq = sp + 128 * 128;
+#pragma unroll
+        for (int u = 0; u < Cfg::U; ++u) {
+          const int r = (tid >> 2) + (u < 2 ? u : u - 2) * 64;
+          if (u < 2)
+            put16(sp, r, c, raw[d][u]);
+          else if (BN >= 64 || r < BN)
+            put16(sq, r, c, raw[d][u]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
+        fetch(i + d + Cfg::DIST, raw[d]);
+        if (++stage == Cfg::STAGES) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+    }
+    if (!mbar_wait(smem_u32(&done), 0, 2 * lim)) atomicCAS(status, 0, -7);
+    tc_fence_after();
+    // the accumulators: rows by the warp's quarter, columns in two halves (one where BN is 16)
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    constexpr int HALF = BN >= 32 ? BN / 2 : 16;
+    const int c0 = (warp >> 2) * HALF;
+    if (splits == 1) {
+      if (c0 < BN) {
+#pragma unroll 1
+        for (int cc = c0; cc < c0 + HALF; cc += 16) {
+          uint32_t r[16];
+          tmem_ld16(trow + (uint32_t)cc, r);
+          tmem_ld_wait();
+          store_y<SWAP>(a, p0 + row, q0 + cc, reinterpret_cast<const float*>(r), 16);
+        }
+      }
+    } else if (c0 < BN) {
+      float* part = reinterpret_cast<float*>(smem);  // [BN][128]: the stages are free
+#pragma unroll 1
+      for (int cc = c0; cc < c0 + HALF; cc += 16) {
+        uint32_t r[16];
+        tmem_ld16(trow + (uint32_t)cc, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[(cc + j) * 128 + row] = nk > 0 ? __uint_as_float(r[j]) : 0.f;
+      }
+    }
+  }
+  if (splits > 1) {
+    cluster_sync();
+    if (warp < 8) {
+      // this rank's share of the columns, eight at a time
+      const int row = tid & 127;
+      for (int g = rank * 2 + (tid >> 7); g * 8 < BN; g += 2 * splits) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        for (int s = 0; s < splits; ++s)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            v[j] += ld_cluster(smem_u32(smem) + (uint32_t)(((g * 8 + j) * 128 + row) * 4), (uint32_t)s);
+        store_y<SWAP>(a, p0 + row, q0 + g * 8, v, 8);
+      }
+    }
+    cluster_sync();  // no CTA leaves while another reads its part
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8 && drained) {
+    tc_fence_after();
+    tmem_dealloc(tmem, Cfg::TMEM);
+  }
+}
+
+namespace {
+
+template <int BN, bool SWAP, bool ALIGNED>
+cudaError_t linear_mma(const LinearI8& a, int splits, int* status, cudaStream_t s) {
+  using Cfg = I8Cfg<BN>;
+  auto kernel = k_linear_i8_mma<BN, SWAP, ALIGNED>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM);
+  if (e != cudaSuccess) return e;
+  const int P = SWAP ? a.n : a.m, Q = SWAP ? a.m : a.n;
+  const int q_tiles = (Q + BN - 1) / BN;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((P + 127) / 128) * (unsigned)q_tiles * (unsigned)splits);
+  cfg.blockDim = dim3(kI8Threads);
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, kernel, a, q_tiles, splits, status, 4000000000ull);
   return e == cudaSuccess ? counted_launches(1) : e;
+}
+
+template <int BN, bool SWAP>
+cudaError_t linear_al(const LinearI8& a, int splits, int* status, cudaStream_t s) {
+  return (a.k & 15) == 0 ? linear_mma<BN, SWAP, true>(a, splits, status, s)
+                         : linear_mma<BN, SWAP, false>(a, splits, status, s);
+}
+
+template <int MT>
+cudaError_t linear_rows(const LinearI8& a, cudaStream_t s) {
+  const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)((a.m + MT - 1) / MT));
+  const cudaError_t e = (a.k & 15) == 0 ? launch_pdl(k_linear_i8_rows<MT, true>, grid, dim3(256), 0, s, a)
+                                        : launch_pdl(k_linear_i8_rows<MT, false>, grid, dim3(256), 0, s, a);
+  return e == cudaSuccess ? counted_launches(1) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s) {
+  if (a.m == 1) return linear_rows<1>(a, s);
+  if (a.m == 2) return linear_rows<2>(a, s);
+  if (a.m <= 4) return linear_rows<4>(a, s);
+  if (a.m <= 8) return linear_rows<8>(a, s);
+  const bool swap = a.m <= 64;
+  const long long P = swap ? a.n : a.m, Q = swap ? a.m : a.n;
+  const long long pt = (P + 127) / 128;
+  int bn = Q <= 16 ? 16 : Q <= 32 ? 32 : Q <= 64 ? 64 : Q <= 128 ? 128 : 256;
+  if (bn == 256 && pt * ((Q + 255) / 256) < sms) bn = 128;
+  if (bn == 128 && pt * ((Q + 127) / 128) < sms) bn = 64;
+  const long long tiles = pt * ((Q + bn - 1) / bn);
+  const int kbs = (a.k + 63) / 64;
+  int splits = 1;
+  if (bn <= 64)
+    while (splits < 8 && tiles * splits * 2 <= 2 * sms && kbs >= splits * 8) splits *= 2;
+  switch (bn) {
+    case 16: return linear_al<16, true>(a, splits, status, s);
+    case 32: return linear_al<32, true>(a, splits, status, s);
+    case 64: return swap ? linear_al<64, true>(a, splits, status, s) : linear_al<64, false>(a, splits, status, s);
+    case 128: return linear_al<128, false>(a, splits, status, s);
+    default: return linear_al<256, false>(a, splits, status, s);
+  }
 }
 
 }  // namespace pf16
