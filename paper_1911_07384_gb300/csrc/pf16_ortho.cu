@@ -47,7 +47,8 @@ constexpr float kSx = 32768.f, kSa = 32768.f, kSb = 16384.f;
 constexpr int kStages = 6;
 constexpr int kStageBytes = 4 * kOrthoBlk;  // two blocks of each operand
 constexpr int kRing = 4;                    // work items in flight inside a CTA
-constexpr int kThreads = 192;               // producer, MMA, four epilogue warps
+constexpr int kEpi = 256;                   // epilogue threads: two warps for each quarter of the accumulator's rows
+constexpr int kThreads = 64 + kEpi;         // and a warp each for the loads and the MMAs
 constexpr int kPackPitch = 65;
 constexpr int kOrthoSmem = 1024 + kStages * kStageBytes + kStageBytes + 256;
 
@@ -71,7 +72,7 @@ __device__ __forceinline__ void bulk_store_1d(void* dst, uint32_t src, uint32_t 
                "r"(src), "r"(bytes)
                : "memory");
 }
-__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 __device__ __forceinline__ float h2f(uint16_t h) { return __half2float(__ushort_as_half(h)); }
 __device__ __forceinline__ uint16_t f2h(float f) { return __half_as_ushort(__float2half_rn(f)); }
@@ -226,38 +227,74 @@ __global__ void __launch_bounds__(256) k_ortho_norm(const __grid_constant__ Orth
 
 namespace {
 
-// 1 / |U|_F from the matrix's partial sums, the same in all 128 threads.  A zero
+// 1 / |U|_F from the matrix's partial sums, the same in all epilogue threads.  A zero
 // matrix gives 0 (its result is zero); a norm that is not finite gives NaN, and
 // with it a result of NaNs only.
 __device__ __forceinline__ float inv_norm(const OrthoParams& p, const OrthoMat& M, float* red, int t) {
   float s = 0.f;
-  for (int i = t; i < M.parts; i += 128) s += __ldcg(p.parts + M.part0 + i);
+  for (int i = t; i < M.parts; i += kEpi) s += __ldcg(p.parts + M.part0 + i);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
   if ((t & 31) == 0) red[t >> 5] = s;
   epi_barrier();
-  s = (red[0] + red[1]) + (red[2] + red[3]);
+  s = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
   if (s == 0.f) return 0.f;
   if (!(s <= 3.402823466e38f)) return __int_as_float(0x7fffffff);
   return 1.f / sqrtf(s);
 }
 
-// One 64 x 64 block of X0, FP32 and scaled binary16.  128 threads.
-__device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int bj, float* tile, float* red, int t) {
-  const float inv = inv_norm(p, M, red, t);
+// One 64 x 64 block of X0, FP32 and scaled binary16, by the epilogue threads.  The loads are
+// in flight while the norm is summed.
+__device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int bj, float* tile, float* red, int t,
+                           int& inv_mat, float& inv, int mat) {
   const int r0 = M.tall ? bj * 64 : bi * 64, c0 = M.tall ? bi * 64 : bj * 64;  // in the caller's matrix
-#pragma unroll 8
-  for (int i = 0; i < 32; ++i) {
-    const int rr = i * 2 + (t >> 6), cc = t & 63;
-    float u = 0.f;
-    if (r0 + rr < M.rows && c0 + cc < M.cols) {
-      const long long at = (long long)(r0 + rr) * M.cols + (c0 + cc);
-      u = h2f(M.g[at]);
-      if (p.muon) u = ortho_u(p, u, h2f(__ldcg(M.v + at)));
-      u *= inv;
-      if (inv != inv) u = inv;
+  float u[16];
+  const bool vec = (M.cols & 7) == 0;
+  if (vec) {  // rows of whole vectors: eight elements a load
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int rr = i * 32 + (t >> 3), cc = (t & 7) * 8;
+      uint4 g = make_uint4(0, 0, 0, 0), v = g;
+      if (r0 + rr < M.rows && c0 + cc < M.cols) {
+        const long long at = (long long)(r0 + rr) * M.cols + (c0 + cc);
+        g = __ldg(reinterpret_cast<const uint4*>(M.g + at));
+        if (p.muon) v = __ldcg(reinterpret_cast<const uint4*>(M.v + at));
+      }
+      const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, vw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float2 x = h22f(gw[j]);
+        if (p.muon) {
+          const float2 y = h22f(vw[j]);
+          x.x = ortho_u(p, x.x, y.x);
+          x.y = ortho_u(p, x.y, y.y);
+        }
+        u[i * 8 + 2 * j] = x.x;
+        u[i * 8 + 2 * j + 1] = x.y;
+      }
     }
-    tile[M.tall ? cc * kPackPitch + rr : rr * kPackPitch + cc] = u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int rr = i * 4 + (t >> 6), cc = t & 63;
+      u[i] = 0.f;
+      if (r0 + rr < M.rows && c0 + cc < M.cols) {
+        const long long at = (long long)(r0 + rr) * M.cols + (c0 + cc);
+        u[i] = h2f(__ldg(M.g + at));
+        if (p.muon) u[i] = ortho_u(p, u[i], h2f(__ldcg(M.v + at)));
+      }
+    }
+  }
+  if (inv_mat != mat) {
+    inv = inv_norm(p, M, red, t);
+    inv_mat = mat;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int rr = vec ? (i >> 3) * 32 + (t >> 3) : i * 4 + (t >> 6), cc = vec ? (t & 7) * 8 + (i & 7) : t & 63;
+    float x = u[i] * inv;
+    if (inv != inv) x = r0 + rr < M.rows && c0 + cc < M.cols ? inv : 0.f;
+    tile[M.tall ? cc * kPackPitch + rr : rr * kPackPitch + cc] = x;
   }
   epi_barrier();
   const OrthoLayout L = ortho_layout(M.mb, M.nb);
@@ -265,74 +302,85 @@ __device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int 
   uint8_t* x32 = M.ws + L.x32 + blk * (2 * kOrthoBlk);
   uint8_t* x16 = M.ws + L.x16 + blk * kOrthoBlk;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = t & 63, c4 = (t >> 6) + 2 * i;
+  for (int i = 0; i < 4; ++i) {
+    const int row = t & 63, c4 = (t >> 6) + 4 * i;
     const float* s = tile + row * kPackPitch + c4 * 4;
-    *reinterpret_cast<float4*>(x32 + (c4 * 64 + row) * 16) = make_float4(s[0], s[1], s[2], s[3]);
+    __stcg(reinterpret_cast<float4*>(x32 + (c4 * 64 + row) * 16), make_float4(s[0], s[1], s[2], s[3]));
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = (t >> 3) + 16 * i, ch = t & 7;
+  for (int i = 0; i < 2; ++i) {
+    const int row = (t >> 3) + 32 * i, ch = t & 7;
     const float* s = tile + row * kPackPitch + ch * 8;
     uint4 v;
     v.x = f2h2(s[0] * kSx, s[1] * kSx);
     v.y = f2h2(s[2] * kSx, s[3] * kSx);
     v.z = f2h2(s[4] * kSx, s[5] * kSx);
     v.w = f2h2(s[6] * kSx, s[7] * kSx);
-    *reinterpret_cast<uint4*>(x16 + row * 128 + ((ch ^ (row & 7)) << 4)) = v;
+    __stcg(reinterpret_cast<uint4*>(x16 + row * 128 + ((ch ^ (row & 7)) << 4)), v);
   }
 }
 
-// The final step's 16 columns [c, c + 16) of inner row r: written to the caller's output, or
-// the weights' step taken with them.
-__device__ __forceinline__ void finish16(const OrthoParams& p, const OrthoMat& M, int r, int c, const float* x) {
+__device__ __forceinline__ float muon_w(const OrthoParams& p, const OrthoMat& M, float w, float x) {
+  return w - p.lr * fmaf(M.scale, x, p.wd * w);
+}
+
+// The final step's 64 columns from c on of inner row r: written to the caller's output, or
+// the weights' step taken with them (their loads all issued first).
+__device__ __forceinline__ void finish64(const OrthoParams& p, const OrthoMat& M, int r, int c, const float* x) {
   if (M.tall) {  // inner row r is the caller's column: neighbouring lanes write neighbouring elements
     if (r >= M.cols) return;
+    uint16_t* o = M.w + (long long)c * M.cols + r;
+    const int left = M.rows - c;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      if (c + j >= M.rows) break;
-      uint16_t* o = M.w + (long long)(c + j) * M.cols + r;
+    for (int h = 0; h < 64; h += 32) {
+      float w[32];
       if (p.muon) {
-        const float w = h2f(*o);
-        *o = f2h(w - p.lr * fmaf(M.scale, x[j], p.wd * w));
-      } else {
-        *o = f2h(x[j]);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) w[j] = h + j < left ? h2f(o[(long long)(h + j) * M.cols]) : 0.f;
       }
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (h + j < left) o[(long long)(h + j) * M.cols] = f2h(p.muon ? muon_w(p, M, w[j], x[h + j]) : x[h + j]);
     }
     return;
   }
   if (r >= M.rows) return;
   uint16_t* o = M.w + (long long)r * M.cols + c;
+  const int left = M.cols - c;
   if ((M.cols & 7) == 0) {
+    uint4 v[8];
+    if (p.muon) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (c + 8 * h >= M.cols) break;
-      uint4 v;
-      uint32_t* q = reinterpret_cast<uint32_t*>(&v);
-      if (p.muon) v = *reinterpret_cast<const uint4*>(o + 8 * h);
+      for (int h = 0; h < 8; ++h)
+        v[h] = h * 8 < left ? *reinterpret_cast<const uint4*>(o + 8 * h) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      uint32_t q[4] = {v[h].x, v[h].y, v[h].z, v[h].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float2 y = make_float2(x[8 * h + 2 * j], x[8 * h + 2 * j + 1]);
         if (p.muon) {
           const float2 w = h22f(q[j]);
-          y.x = w.x - p.lr * fmaf(M.scale, y.x, p.wd * w.x);
-          y.y = w.y - p.lr * fmaf(M.scale, y.y, p.wd * w.y);
+          y.x = muon_w(p, M, w.x, y.x);
+          y.y = muon_w(p, M, w.y, y.y);
         }
         q[j] = f2h2(y.x, y.y);
       }
-      *reinterpret_cast<uint4*>(o + 8 * h) = v;
+      if (h * 8 < left) *reinterpret_cast<uint4*>(o + 8 * h) = make_uint4(q[0], q[1], q[2], q[3]);
     }
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    if (c + j >= M.cols) break;
+  for (int h = 0; h < 64; h += 32) {
+    float w[32];
     if (p.muon) {
-      const float w = h2f(o[j]);
-      o[j] = f2h(w - p.lr * fmaf(M.scale, x[j], p.wd * w));
-    } else {
-      o[j] = f2h(x[j]);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) w[j] = h + j < left ? h2f(o[h + j]) : 0.f;
     }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (h + j < left) o[h + j] = f2h(p.muon ? muon_w(p, M, w[j], x[h + j]) : x[h + j]);
   }
 }
 
@@ -353,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
   __shared__ Item ring[kRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s, drained;
-  __shared__ float red[4];
+  __shared__ float red[kEpi / 32];
   volatile int* abort_flag = &abort_s;
   const int warp = (int)threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -363,11 +411,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
     }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&item_full[i]), 1);
-      mbar_init(smem_u32(&item_empty[i]), 5);  // the MMA thread and four epilogue warps
+      mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32);  // the MMA thread and the epilogue warps
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&acc_full[i]), 1);
-      mbar_init(smem_u32(&acc_empty[i]), 4);
+      mbar_init(smem_u32(&acc_empty[i]), kEpi / 32);
     }
     mbar_init(smem_u32(&last), 1);
     abort_s = 0;
@@ -528,10 +576,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
       }
     }
   } else {
-    const int t = (int)threadIdx.x - 64;  // 0..127
+    const int t = (int)threadIdx.x - 64;
     const int lane = t & 31, quad = warp & 3;
     const int row = quad * 32 + lane;     // of the tile (TMEM lane)
-    int slot = 0, acc = 0;
+    const int half = t >> 7;              // its columns, 64 of them
+    const int rr = row & 63;
+    int slot = 0, acc = 0, inv_mat = -1;
+    float inv = 0.f;
     uint32_t rphase = 0, aphase = 0;
     while (true) {
       if (!mbar_wait(smem_u32(&item_full[slot]), rphase, 2 * lim)) {
@@ -548,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
       if (it.kind == kStop) break;
       const OrthoMat& M = p.mat[it.mat];
       if (it.kind == kPack) {
-        pack_block(p, M, it.I, it.J, reinterpret_cast<float*>(staging), red, t);
+        pack_block(p, M, it.I, it.J, reinterpret_cast<float*>(staging), red, t, inv_mat, inv, it.mat);
         fence_proxy_async_all();
         epi_barrier();
         if (t == 0) {
@@ -557,69 +608,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
         }
         continue;
       }
+      const OrthoLayout L = ortho_layout(M.mb, M.nb);
+      const bool full_kind = it.kind == kFull;
+      const bool final_step = full_kind && it.step == p.steps - 1;
+      const int ncb = full_kind ? M.nb : M.mb;  // block columns of the result
+      const int bi = it.I * 2 + (row >> 6), bj = it.J * 2 + half;
+      const bool in = bi < M.mb && bj < ncb;
+      // what the result adds to the product, loaded while the product runs (the
+      // item's dependency, which the loading warp has seen, covers it)
+      float x[64];
+      float4* x32 = reinterpret_cast<float4*>(M.ws + L.x32 + ((size_t)bi * M.nb + bj) * (2 * kOrthoBlk)) + rr;
+      if (full_kind) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float4 o = in ? __ldcg(x32 + j * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
+          x[4 * j] = kA * o.x;
+          x[4 * j + 1] = kA * o.y;
+          x[4 * j + 2] = kA * o.z;
+          x[4 * j + 3] = kA * o.w;
+        }
+      } else if (it.kind == kSym2) {
+        const uint8_t* src = M.ws + L.a16 + ((size_t)bi * M.mb + bj) * kOrthoBlk + rr * 128;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint4 o = in ? __ldcg(reinterpret_cast<const uint4*>(src + ((j ^ (rr & 7)) << 4)))
+                             : make_uint4(0, 0, 0, 0);
+          const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float2 f = h22f(ow[q]);
+            x[8 * j + 2 * q] = f.x * (kB * kSb / kSa);
+            x[8 * j + 2 * q + 1] = f.y * (kB * kSb / kSa);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 64; ++j) x[j] = 0.f;
+      }
       if (!mbar_wait(smem_u32(&acc_full[acc]), aphase, 2 * lim)) {
         record_timeout(p.status, abort_flag);
         break;
       }
       tc_fence_after();
-      const OrthoLayout L = ortho_layout(M.mb, M.nb);
-      const bool full_kind = it.kind == kFull;
-      const bool final_step = full_kind && it.step == p.steps - 1;
-      const int ncb = full_kind ? M.nb : M.mb;  // block columns of the result
-      const int bi = it.I * 2 + (row >> 6), rr = row & 63;
-      const uint8_t* A = M.ws + L.a16;
-      uint8_t* X32 = M.ws + L.x32;
-#pragma unroll 1
-      for (int c = 0; c < 128; c += 16) {
-        const int bj = it.J * 2 + (c >> 6), cc = c & 63;
-        const bool in = bi < M.mb && bj < ncb;
-        uint32_t r[16];
-        tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 128 + c), r);
-        float x[16];
-        if (it.kind == kSym1) {
-          tmem_ld_wait();
+      const float mul = it.kind == kSym1   ? kSa / (kSx * kSx)
+                        : it.kind == kSym2 ? kC * kSb / (kSa * kSa)
+                                           : 1.f / (kSx * kSb);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(r[j]) * (kSa / (kSx * kSx));
-        } else if (it.kind == kSym2) {
-          uint4 a[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-          if (in) {
-            const uint8_t* src = A + ((size_t)bi * M.mb + bj) * kOrthoBlk + rr * 128;
-            a[0] = __ldcg(reinterpret_cast<const uint4*>(src + (((cc >> 3) ^ (rr & 7)) << 4)));
-            a[1] = __ldcg(reinterpret_cast<const uint4*>(src + ((((cc >> 3) + 1) ^ (rr & 7)) << 4)));
-          }
-          const uint32_t* ah = reinterpret_cast<const uint32_t*>(a);
-          tmem_ld_wait();
+      for (int c = 0; c < 64; c += 32) {
+        uint32_t r[32];
+        tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 128 + half * 64 + c), r);
+        tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 128 + half * 64 + c + 16), r + 16);
+        tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 av = h22f(ah[j]);
-            x[2 * j] = fmaf(__uint_as_float(r[2 * j]), kC * kSb / (kSa * kSa), av.x * (kB * kSb / kSa));
-            x[2 * j + 1] = fmaf(__uint_as_float(r[2 * j + 1]), kC * kSb / (kSa * kSa), av.y * (kB * kSb / kSa));
-          }
-        } else {
-          float4* src = reinterpret_cast<float4*>(X32 + ((size_t)bi * M.nb + bj) * (2 * kOrthoBlk)) + (cc >> 2) * 64 + rr;
-          float4 o[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = in ? __ldcg(src + j * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
-          tmem_ld_wait();
-          const float* of = reinterpret_cast<const float*>(o);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = fmaf(kA, of[j], __uint_as_float(r[j]) * (1.f / (kSx * kSb)));
-          if (final_step) {
-            if (in) finish16(p, M, it.I * 128 + row, it.J * 128 + c, x);
-            continue;
-          }
+        for (int j = 0; j < 32; ++j) x[c + j] = fmaf(__uint_as_float(r[j]), mul, x[c + j]);
+      }
+      if (final_step) {
+        if (in) finish64(p, M, it.I * 128 + row, it.J * 128 + half * 64, x);
+      } else {
+        if (full_kind) {
           if (in) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              __stcg(src + j * 64, make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
+            for (int j = 0; j < 16; ++j)
+              __stcg(x32 + j * 64, make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
           }
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] *= kSx;
+          for (int j = 0; j < 64; ++j) x[j] *= kSx;
         }
-        const uint32_t st = smem_u32(staging) + (uint32_t)(((row >> 6) * 2 + (c >> 6)) * kOrthoBlk + rr * 128);
+        const uint32_t st = smem_u32(staging) + (uint32_t)(((row >> 6) * 2 + half) * kOrthoBlk + rr * 128);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          st_shared_v4(st + (uint32_t)((((cc >> 3) + h) ^ (rr & 7)) << 4),
+        for (int h = 0; h < 8; ++h)
+          st_shared_v4(st + (uint32_t)((h ^ (rr & 7)) << 4),
                        make_uint4(f2h2(x[8 * h], x[8 * h + 1]), f2h2(x[8 * h + 2], x[8 * h + 3]),
                                   f2h2(x[8 * h + 4], x[8 * h + 5]), f2h2(x[8 * h + 6], x[8 * h + 7])));
       }
