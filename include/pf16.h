@@ -410,7 +410,7 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  * FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
  * norm is not finite gives NaNs throughout.  Same inputs, same bits.
  *
- * All matrices of one call run together, in two launches.  1 <= rows, cols <=
+ * All matrices of one call run together, in three launches.  1 <= rows, cols <=
  * 65536, rows * cols <= 2^30, at most PF16_ORTHO_MAX_MATRICES matrices
  * (PF16_ERR_UNSUPPORTED beyond), 1 <= steps <= 16 (PF16_ERR_ARG).  The list
  * is host memory, read before the call returns.  Arrays are dense, row-major,

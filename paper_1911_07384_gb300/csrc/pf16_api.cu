@@ -1677,9 +1677,8 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   p->count = count;
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
-  size_t at = round_up(16 + (size_t)count * 4, 256);
-  p->parts = reinterpret_cast<float*>(base + at);
-  long long parts = 0, pack = 0, sym = 0, full = 0;
+  size_t words = 4 + (size_t)count;
+  long long parts = 0, pack = 0, gram = 0, sym = 0, full = 0, blocks = 0;
   for (int i = 0; i < count; ++i) {
     const OrthoEntry& s = e[order[i]];
     OrthoMat& m = p->mat[i];
@@ -1695,23 +1694,41 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     m.part0 = (int)parts;
     m.parts = ortho_parts((long long)s.rows * s.cols);
     parts += m.parts;
-    const int mt = cdiv(m.mb, 2), nt = cdiv(m.nb, 2);
+    blocks += (long long)ortho_sym(ortho_tiles(m.mb)) * m.nb;
+  }
+  // X X^T's sums split so that an item's share is near a pair's share of them all, but no less
+  // than 12 blocks (about 3 us: a part costs its store and the last one all loads).
+  const long long share = std::max(12ll, blocks / kOrthoPairs);
+  for (int i = 0; i < count; ++i) {
+    OrthoMat& m = p->mat[i];
+    m.splits = (int)std::min<long long>(8, std::max<long long>(1, m.nb / share));
+    m.kper = cdiv(m.nb, m.splits);
+    m.splits = cdiv(m.nb, m.kper);
+    const int mt = ortho_tiles(m.mb), nt = ortho_tiles(m.nb), tri = ortho_sym(mt);
+    m.arrivals = p->ticket + words;
+    if (m.splits > 1) words += (size_t)tri * kOrthoSignals;
     p->pre_pack[i] = (int)pack;
+    p->pre_gram[i] = (int)gram;
     p->pre_sym[i] = (int)sym;
     p->pre_full[i] = (int)full;
     pack += (long long)m.mb * m.nb;
-    sym += (long long)mt * (mt + 1) / 2;
+    gram += (long long)tri * m.splits;
+    sym += tri;
     full += (long long)mt * nt;
   }
   p->pre_pack[count] = (int)pack;
+  p->pre_gram[count] = (int)gram;
   p->pre_sym[count] = (int)sym;
   p->pre_full[count] = (int)full;
   p->total_parts = (int)parts;
-  p->max_items = (int)std::max(std::max(pack, sym), full);
+  p->max_items = (int)std::max(gram, full);
+  p->zero_words = words;
+  size_t at = round_up(words * 4, 256);
+  p->parts = reinterpret_cast<float*>(base + at);
   at += round_up((size_t)parts * 4, 256);
   for (int i = 0; i < count; ++i) {
     p->mat[i].ws = base + at;
-    at += ortho_layout(p->mat[i].mb, p->mat[i].nb).bytes;
+    at += ortho_layout(p->mat[i].mb, p->mat[i].nb, p->mat[i].splits).bytes;
   }
   return at;
 }

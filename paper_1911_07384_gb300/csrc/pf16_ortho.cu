@@ -23,12 +23,19 @@
 // and below the diagonal are computed and stored.  The caller's arrays, of any
 // size and alignment of rows, are touched by the first and last phase only.
 //
-// Schedule.  One persistent kernel runs all phases of all matrices: work items
-// (a block to pack, a 128 x 128 tile of a product) are numbered phase by phase
+// Tiles.  A product's tile is 256 x 256, made by a pair of CTAs with
+// tcgen05.mma.cta_group::2: each CTA loads 128 rows of either operand, 64 bytes
+// a clock at the full MMA rate.  128 x 128 tiles of single CTAs need 128 and were
+// bound by the L2's 46 bytes a clock and SM (4096 x 4096: 2.34 ms).
+// X X^T of a wide matrix has few tiles and long sums: the sum is split over n,
+// and the part that arrives last adds all parts in order.
+//
+// Schedule.  After the norms and the packing, one persistent kernel runs all
+// phases of all matrices: work items (tiles of a product) are numbered phase by phase
 // and handed out by an atomic ticket, and an item starts once the item count of
 // its matrix shows the previous phase complete.  An item waits only for items
-// with smaller tickets, which running CTAs hold, so the kernel makes progress
-// with any number of its CTAs resident.
+// with smaller tickets, which running pairs hold, so the kernel makes progress
+// with any number of its pairs resident.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -45,16 +52,17 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kSx = 32768.f, kSa = 32768.f, kSb = 16384.f;
 
 constexpr int kStages = 6;
-constexpr int kStageBytes = 4 * kOrthoBlk;  // two blocks of each operand
-constexpr int kRing = 4;                    // work items in flight inside a CTA
+constexpr int kStageBytes = 4 * kOrthoBlk;  // a CTA's two blocks of each operand
+constexpr int kRing = 4;                    // work items in flight inside a pair
 constexpr int kEpi = 256;                   // epilogue threads: two warps for each quarter of the accumulator's rows
 constexpr int kThreads = 64 + kEpi;         // and a warp each for the loads and the MMAs
 constexpr int kPackPitch = 65;
-constexpr int kOrthoSmem = 1024 + kStages * kStageBytes + kStageBytes + 256;
+constexpr int kOrthoSmem = 1024 + kStages * kStageBytes + 4 * kOrthoBlk;
 
-enum ItemKind : int { kPack = 0, kSym1 = 1, kSym2 = 2, kFull = 3, kStop = 4 };
-struct Item {
-  int kind, mat, I, J, step;
+enum ItemKind : int { kGram = 1, kSym = 2, kFull = 3, kStop = 4 };
+struct __align__(16) Item {
+  int kind, mat, I, J;
+  int step, k0, k1, split;  // blocks [k0, k1) of the sum, which part of it
 };
 
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
@@ -72,7 +80,6 @@ __device__ __forceinline__ void bulk_store_1d(void* dst, uint32_t src, uint32_t 
                "r"(src), "r"(bytes)
                : "memory");
 }
-__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 __device__ __forceinline__ float h2f(uint16_t h) { return __half2float(__ushort_as_half(h)); }
 __device__ __forceinline__ uint16_t f2h(float f) { return __half_as_ushort(__float2half_rn(f)); }
@@ -97,58 +104,132 @@ __device__ __forceinline__ int find_mat(const int* pre, int n, int t) {
   return lo;
 }
 
-__device__ __forceinline__ int sym_tiles(int mt) { return mt * (mt + 1) / 2; }
+// row and column of tile `local` of a lower triangle, whose row I holds tiles I(I+1)/2 .. I(I+1)/2 + I
+__device__ __forceinline__ void sym_tile(int local, int& I, int& J) {
+  I = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
+  while (ortho_sym(I) > local) --I;
+  while (ortho_sym(I + 1) <= local) ++I;
+  J = local - ortho_sym(I);
+}
 
-// Ticket -> work item, and the number of finished items of its matrix that it waits for.
+// Ticket -> work item, and the count of its matrix that it waits for.
 __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, uint32_t& need) {
   Item it;
   const int n = p.count;
-  const int tp = p.pre_pack[n], ts = p.pre_sym[n], tf = p.pre_full[n];
-  need = 0;
-  it.step = 0;
-  if (ticket < (uint32_t)tp) {
-    it.kind = kPack;
-    it.mat = find_mat(p.pre_pack, n, (int)ticket);
-    const int local = (int)ticket - p.pre_pack[it.mat];
-    it.I = local / p.mat[it.mat].nb;
-    it.J = local % p.mat[it.mat].nb;
-    return it;
-  }
-  uint32_t t = ticket - (uint32_t)tp;
-  const uint32_t per = (uint32_t)(2 * ts + tf);
+  const int tg = p.pre_gram[n], ts = p.pre_sym[n], tf = p.pre_full[n];
+  it.k0 = it.split = 0;
+  uint32_t t = ticket;
+  const uint32_t per = (uint32_t)(tg + ts + tf);
   it.step = (int)(t / per);
   t -= (uint32_t)it.step * per;
   if (it.step >= p.steps) {
     it.kind = kStop;
-    it.mat = it.I = it.J = 0;
+    it.mat = it.I = it.J = it.k1 = 0;
+    need = 0;
     return it;
   }
-  if (t < (uint32_t)(2 * ts)) {
-    it.kind = t < (uint32_t)ts ? kSym1 : kSym2;
-    if (it.kind == kSym2) t -= (uint32_t)ts;
+  if (t < (uint32_t)tg) {
+    it.kind = kGram;
+    it.mat = find_mat(p.pre_gram, n, (int)t);
+    const OrthoMat& M = p.mat[it.mat];
+    const int local = (int)t - p.pre_gram[it.mat];
+    it.split = local % M.splits;
+    sym_tile(local / M.splits, it.I, it.J);
+    it.k0 = it.split * M.kper;
+    it.k1 = min(it.k0 + M.kper, M.nb);
+  } else if (t < (uint32_t)(tg + ts)) {
+    t -= (uint32_t)tg;
+    it.kind = kSym;
     it.mat = find_mat(p.pre_sym, n, (int)t);
-    const int local = (int)t - p.pre_sym[it.mat];
-    // row I of the lower triangle holds tiles I(I+1)/2 .. I(I+1)/2 + I
-    int I = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
-    while (sym_tiles(I) > local) --I;
-    while (sym_tiles(I + 1) <= local) ++I;
-    it.I = I;
-    it.J = local - sym_tiles(I);
+    sym_tile((int)t - p.pre_sym[it.mat], it.I, it.J);
+    it.k1 = p.mat[it.mat].mb;
   } else {
-    t -= (uint32_t)(2 * ts);
+    t -= (uint32_t)(tg + ts);
     it.kind = kFull;
     it.mat = find_mat(p.pre_full, n, (int)t);
     const int local = (int)t - p.pre_full[it.mat];
-    const int mt = (p.mat[it.mat].mb + 1) >> 1;
+    const int mt = ortho_tiles(p.mat[it.mat].mb);
     it.I = local % mt;  // column by column: neighbours share X's blocks
     it.J = local / mt;
+    it.k1 = p.mat[it.mat].mb;
   }
   const OrthoMat& M = p.mat[it.mat];
-  const int mt = (M.mb + 1) >> 1, nt = (M.nb + 1) >> 1;
-  const uint32_t sym = (uint32_t)sym_tiles(mt);
-  need = (uint32_t)(M.mb * M.nb) + (uint32_t)it.step * (2 * sym + (uint32_t)(mt * nt)) +
-         (uint32_t)(it.kind - kSym1) * sym;
+  const int mt = ortho_tiles(M.mb), nt = ortho_tiles(M.nb);
+  const uint32_t sym = (uint32_t)ortho_sym(mt);
+  need = kOrthoSignals * ((uint32_t)it.step * (2 * sym + (uint32_t)(mt * nt)) + (uint32_t)(it.kind - kGram) * sym);
   return it;
+}
+
+// ---------------------------------------------------------------------------
+// The pair of CTAs
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_rank(uint32_t saddr, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
+  return a;
+}
+// arrive on a barrier of either CTA (an address from map_rank)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t mapped) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t mapped, int a, int b, int c, int d) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mapped), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// mbar_wait for a barrier that the other CTA arrives on
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i)
+      if (mbar_try_wait_cluster(bar, parity)) return true;
+    if (globaltimer_ns() - t0 > limit_ns) return false;
+  }
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t dst_smem, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+// 256 rows of A, 128 in each CTA, against N columns of B, N / 2 in each CTA
+__device__ __forceinline__ void tc_mma_f16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                                uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
+      : "memory");
+}
+// an arrival on the barrier at this address in both CTAs once the MMAs issued so far complete
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
 }
 
 }  // namespace
@@ -165,10 +246,7 @@ __device__ __forceinline__ float ortho_u(const OrthoParams& p, float g, float v)
 __global__ void __launch_bounds__(256) k_ortho_norm(const __grid_constant__ OrthoParams p) {
   pdl_wait();
   const int tid = (int)threadIdx.x;
-  if (blockIdx.x == 0) {
-    if (tid == 0) *p.ticket = 0;
-    for (int i = tid; i < p.count; i += 256) p.done[i] = 0;
-  }
+  for (size_t i = (size_t)blockIdx.x * 256 + tid; i < p.zero_words; i += (size_t)gridDim.x * 256) p.ticket[i] = 0;
   // the matrix whose partial sums hold this block
   int lo = 0, hi = p.count;
   while (hi - lo > 1) {
@@ -227,26 +305,34 @@ __global__ void __launch_bounds__(256) k_ortho_norm(const __grid_constant__ Orth
 
 namespace {
 
-// 1 / |U|_F from the matrix's partial sums, the same in all epilogue threads.  A zero
+// 1 / |U|_F from the matrix's partial sums, the same in all threads.  A zero
 // matrix gives 0 (its result is zero); a norm that is not finite gives NaN, and
 // with it a result of NaNs only.
 __device__ __forceinline__ float inv_norm(const OrthoParams& p, const OrthoMat& M, float* red, int t) {
   float s = 0.f;
-  for (int i = t; i < M.parts; i += kEpi) s += __ldcg(p.parts + M.part0 + i);
+  for (int i = t; i < M.parts; i += 256) s += p.parts[M.part0 + i];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
   if ((t & 31) == 0) red[t >> 5] = s;
-  epi_barrier();
+  __syncthreads();
   s = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
   if (s == 0.f) return 0.f;
   if (!(s <= 3.402823466e38f)) return __int_as_float(0x7fffffff);
   return 1.f / sqrtf(s);
 }
 
-// One 64 x 64 block of X0, FP32 and scaled binary16, by the epilogue threads.  The loads are
-// in flight while the norm is summed.
-__device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int bj, float* tile, float* red, int t,
-                           int& inv_mat, float& inv, int mat) {
+}  // namespace
+
+// Each CTA makes one 64 x 64 block of X0, FP32 and scaled binary16.  The loads are in
+// flight while the norm is summed.
+__global__ void __launch_bounds__(256) k_ortho_pack(const __grid_constant__ OrthoParams p) {
+  __shared__ float tile[64 * kPackPitch];
+  __shared__ float red[8];
+  pdl_wait();
+  const int t = (int)threadIdx.x;
+  const int mat = find_mat(p.pre_pack, p.count, (int)blockIdx.x);
+  const OrthoMat& M = p.mat[mat];
+  const int bi = ((int)blockIdx.x - p.pre_pack[mat]) / M.nb, bj = ((int)blockIdx.x - p.pre_pack[mat]) % M.nb;
   const int r0 = M.tall ? bj * 64 : bi * 64, c0 = M.tall ? bi * 64 : bj * 64;  // in the caller's matrix
   float u[16];
   const bool vec = (M.cols & 7) == 0;
@@ -285,10 +371,7 @@ __device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int 
       }
     }
   }
-  if (inv_mat != mat) {
-    inv = inv_norm(p, M, red, t);
-    inv_mat = mat;
-  }
+  const float inv = inv_norm(p, M, red, t);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int rr = vec ? (i >> 3) * 32 + (t >> 3) : i * 4 + (t >> 6), cc = vec ? (t & 7) * 8 + (i & 7) : t & 63;
@@ -296,16 +379,15 @@ __device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int 
     if (inv != inv) x = r0 + rr < M.rows && c0 + cc < M.cols ? inv : 0.f;
     tile[M.tall ? cc * kPackPitch + rr : rr * kPackPitch + cc] = x;
   }
-  epi_barrier();
-  const OrthoLayout L = ortho_layout(M.mb, M.nb);
-  const size_t blk = (size_t)bi * M.nb + bj;
-  uint8_t* x32 = M.ws + L.x32 + blk * (2 * kOrthoBlk);
-  uint8_t* x16 = M.ws + L.x16 + blk * kOrthoBlk;
+  __syncthreads();
+  const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
+  uint8_t* x32 = M.ws + L.x32 + ((size_t)bi * M.nb + bj) * (2 * kOrthoBlk);
+  uint8_t* x16 = M.ws + L.x16 + ortho_block(bi, bj, (M.nb + 1) & ~1) * kOrthoBlk;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = t & 63, c4 = (t >> 6) + 4 * i;
     const float* s = tile + row * kPackPitch + c4 * 4;
-    __stcg(reinterpret_cast<float4*>(x32 + (c4 * 64 + row) * 16), make_float4(s[0], s[1], s[2], s[3]));
+    *reinterpret_cast<float4*>(x32 + (c4 * 64 + row) * 16) = make_float4(s[0], s[1], s[2], s[3]);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -316,46 +398,32 @@ __device__ void pack_block(const OrthoParams& p, const OrthoMat& M, int bi, int 
     v.y = f2h2(s[2] * kSx, s[3] * kSx);
     v.z = f2h2(s[4] * kSx, s[5] * kSx);
     v.w = f2h2(s[6] * kSx, s[7] * kSx);
-    __stcg(reinterpret_cast<uint4*>(x16 + row * 128 + ((ch ^ (row & 7)) << 4)), v);
+    *reinterpret_cast<uint4*>(x16 + row * 128 + ((ch ^ (row & 7)) << 4)) = v;
   }
 }
+
+namespace {
 
 __device__ __forceinline__ float muon_w(const OrthoParams& p, const OrthoMat& M, float w, float x) {
   return w - p.lr * fmaf(M.scale, x, p.wd * w);
 }
 
-// The final step's 64 columns from c on of inner row r: written to the caller's output, or
+// The final step's 32 columns from c on of inner row r: written to the caller's output, or
 // the weights' step taken with them (their loads all issued first).
-__device__ __forceinline__ void finish64(const OrthoParams& p, const OrthoMat& M, int r, int c, const float* x) {
-  if (M.tall) {  // inner row r is the caller's column: neighbouring lanes write neighbouring elements
-    if (r >= M.cols) return;
-    uint16_t* o = M.w + (long long)c * M.cols + r;
-    const int left = M.rows - c;
-#pragma unroll
-    for (int h = 0; h < 64; h += 32) {
-      float w[32];
-      if (p.muon) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) w[j] = h + j < left ? h2f(o[(long long)(h + j) * M.cols]) : 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (h + j < left) o[(long long)(h + j) * M.cols] = f2h(p.muon ? muon_w(p, M, w[j], x[h + j]) : x[h + j]);
-    }
-    return;
-  }
-  if (r >= M.rows) return;
-  uint16_t* o = M.w + (long long)r * M.cols + c;
-  const int left = M.cols - c;
-  if ((M.cols & 7) == 0) {
-    uint4 v[8];
+__device__ __forceinline__ void finish32(const OrthoParams& p, const OrthoMat& M, int r, int c, const float* x) {
+  const bool vec = !M.tall && (M.cols & 7) == 0;
+  if (vec) {
+    if (r >= M.rows) return;
+    uint16_t* o = M.w + (long long)r * M.cols + c;
+    const int left = M.cols - c;
+    uint4 v[4];
     if (p.muon) {
 #pragma unroll
-      for (int h = 0; h < 8; ++h)
+      for (int h = 0; h < 4; ++h)
         v[h] = h * 8 < left ? *reinterpret_cast<const uint4*>(o + 8 * h) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int h = 0; h < 8; ++h) {
+    for (int h = 0; h < 4; ++h) {
       uint32_t q[4] = {v[h].x, v[h].y, v[h].z, v[h].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -371,17 +439,20 @@ __device__ __forceinline__ void finish64(const OrthoParams& p, const OrthoMat& M
     }
     return;
   }
+  // single elements: of a row of the caller's, or, where it is tall, of the column r (there
+  // neighbouring lanes write neighbouring elements)
+  if (r >= (M.tall ? M.cols : M.rows)) return;
+  const long long pitch = M.tall ? M.cols : 1;
+  uint16_t* o = M.tall ? M.w + (long long)c * M.cols + r : M.w + (long long)r * M.cols + c;
+  const int left = (M.tall ? M.rows : M.cols) - c;
+  float w[32];
+  if (p.muon) {
 #pragma unroll
-  for (int h = 0; h < 64; h += 32) {
-    float w[32];
-    if (p.muon) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) w[j] = h + j < left ? h2f(o[h + j]) : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (h + j < left) o[h + j] = f2h(p.muon ? muon_w(p, M, w[j], x[h + j]) : x[h + j]);
+    for (int j = 0; j < 32; ++j) w[j] = j < left ? h2f(o[j * pitch]) : 0.f;
   }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < left) o[j * pitch] = f2h(p.muon ? muon_w(p, M, w[j], x[j]) : x[j]);
 }
 
 __device__ __forceinline__ void record_timeout(int* status, volatile int* abort_flag) {
@@ -391,117 +462,168 @@ __device__ __forceinline__ void record_timeout(int* status, volatile int* abort_
 
 }  // namespace
 
-__global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ OrthoParams p) {
+namespace {
+
+// Whether the operand tile `tile` of kind `kind` at block kb comes transposed (MN-major): the
+// right operand of the full product always, a symmetric operand above its diagonal tiles.
+__device__ __forceinline__ bool is_mn(int kind, bool right, int tile, int kb) {
+  if (kind == kGram) return false;
+  if (kind == kFull && right) return true;
+  return (kb >> 2) > tile;
+}
+// The end of the run of blocks from kb on in which both operands keep their form.
+__device__ __forceinline__ int run_end(const Item& it, int kb) {
+  int e = it.k1;
+  if (it.kind == kGram) return e;
+  if ((kb >> 2) <= it.I) e = min(e, it.I * 4 + 4);
+  if (it.kind == kSym && (kb >> 2) <= it.J) e = min(e, it.J * 4 + 4);
+  return e;
+}
+
+// 128 rows of an operand, block after block along the sum: one copy of 16 KB, or, transposed,
+// two of 8 KB.
+struct OperandRun {
+  const uint8_t* at;
+  size_t even, odd;  // to the next block from an even one, from an odd one
+  bool mn, live;
+  __device__ __forceinline__ void start(const uint8_t* grid, int pitch, int row, int kb, bool mn_, bool live_) {
+    mn = mn_;
+    live = live_;
+    at = grid + (mn ? ortho_block(kb, row, pitch) : ortho_block(row, kb, pitch)) * kOrthoBlk;
+    even = mn ? kOrthoBlk : 2 * kOrthoBlk;
+    odd = mn ? (size_t)(2 * pitch - 1) * kOrthoBlk : 2 * kOrthoBlk;
+  }
+  __device__ __forceinline__ void load(uint32_t dst, uint32_t bar, int kb) {
+    if (live) {
+      if (mn) {
+        bulk_load_1d(dst, at, kOrthoBlk, bar);
+        bulk_load_1d(dst + kOrthoBlk, at + 2 * kOrthoBlk, kOrthoBlk, bar);
+      } else {
+        bulk_load_1d(dst, at, 2 * kOrthoBlk, bar);
+      }
+    }
+    at += (kb & 1) ? odd : even;
+  }
+};
+
+}  // namespace
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ OrthoParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* staging = smem + kStages * kStageBytes;
+  // (item_empty and acc_empty are used in the leading CTA only)
   __shared__ uint64_t full[kStages], empty[kStages], item_full[kRing], item_empty[kRing], acc_full[2], acc_empty[2],
       last;
   __shared__ Item ring[kRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s, drained;
-  __shared__ float red[kEpi / 32];
   volatile int* abort_flag = &abort_s;
   const int warp = (int)threadIdx.x >> 5;
+  const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_u32(&full[i]), 1);
+      mbar_init(smem_u32(&full[i]), rank == 0 ? 2 : 1);  // the leading CTA's: both CTAs' operands
       mbar_init(smem_u32(&empty[i]), 1);
     }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&item_full[i]), 1);
-      mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32);  // the MMA thread and the epilogue warps
+      mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32 + 2 + kEpi / 32);  // every reader in both CTAs
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&acc_full[i]), 1);
-      mbar_init(smem_u32(&acc_empty[i]), kEpi / 32);
+      mbar_init(smem_u32(&acc_empty[i]), 2 * kEpi / 32);
     }
     mbar_init(smem_u32(&last), 1);
     abort_s = 0;
     drained = 1;
     fence_mbar_init();
   }
-  if (warp == 1) {
-    tmem_alloc(smem_u32(&tmem_slot), 256);
-    tmem_relinquish();
-  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
+  cluster_sync();
   tc_fence_after();
   pdl_wait();
   const uint32_t tmem = tmem_slot;
-  const uint64_t lim = p.wait_limit_ns;  // for a dependency; the waits inside a CTA may hold one
+  const uint64_t lim = p.wait_limit_ns;  // for a dependency; the waits inside a pair may hold one
 
   if (warp == 0) {
     if (elect_one()) {
       int stage = 0, slot = 0;
       uint32_t phase = 0, rphase = 0, issued = 0;
-      uint32_t ticket = atomicAdd(p.ticket, 1u);
+      uint32_t ticket = rank == 0 ? atomicAdd(p.ticket, 1u) : 0;
       while (true) {
-        uint32_t need;
-        Item it = decode(p, ticket, need);
-        if (it.kind != kStop) ticket = atomicAdd(p.ticket, 1u);  // (its latency passes behind this item)
-        const OrthoMat& M = p.mat[it.mat];
-        if (!mbar_wait(smem_u32(&item_empty[slot]), rphase ^ 1, 3 * lim)) {
-          record_timeout(p.status, abort_flag);
-          break;
-        }
-        if (it.kind != kStop && it.kind != kPack) {
-          const uint32_t* d = p.done + it.mat;
-          if (ld_acquire(d) < need) {
-            const uint64_t t0 = globaltimer_ns();
-            while (ld_acquire(d) < need) {
-              if (*abort_flag || globaltimer_ns() - t0 > lim) {
-                record_timeout(p.status, abort_flag);
-                break;
+        Item it;
+        if (rank == 0) {
+          uint32_t need;
+          it = decode(p, ticket, need);
+          if (it.kind != kStop) ticket = atomicAdd(p.ticket, 1u);  // (its latency passes behind this item)
+          if (!mbar_wait_cluster(smem_u32(&item_empty[slot]), rphase ^ 1, 3 * lim)) {
+            record_timeout(p.status, abort_flag);
+            break;
+          }
+          if (it.kind != kStop) {
+            const uint32_t* d = p.done + it.mat;
+            if (ld_acquire(d) < need) {
+              const uint64_t t0 = globaltimer_ns();
+              while (ld_acquire(d) < need) {
+                if (*abort_flag || globaltimer_ns() - t0 > lim) {
+                  record_timeout(p.status, abort_flag);
+                  break;
+                }
               }
             }
           }
           if (*abort_flag) it.kind = kStop;
+          ring[slot] = it;
+          const uint32_t far = map_rank(smem_u32(&ring[slot]), 1);
+          st_cluster_v4(far, it.kind, it.mat, it.I, it.J);
+          st_cluster_v4(far + 16, it.step, it.k0, it.k1, it.split);
+          mbar_arrive(smem_u32(&item_full[slot]));
+          mbar_arrive_cluster(map_rank(smem_u32(&item_full[slot]), 1));
+        } else {
+          if (!mbar_wait_cluster(smem_u32(&item_full[slot]), rphase, 4 * lim)) {
+            record_timeout(p.status, abort_flag);
+            break;
+          }
+          it = ring[slot];
+          mbar_arrive_cluster(map_rank(smem_u32(&item_empty[slot]), 0));
         }
-        ring[slot] = it;
-        mbar_arrive(smem_u32(&item_full[slot]));
         if (++slot == kRing) {
           slot = 0;
           rphase ^= 1;
         }
         if (it.kind == kStop) break;
-        if (it.kind == kPack) continue;
         fence_proxy_async_all();  // the blocks' writers used both proxies
-        const OrthoLayout L = ortho_layout(M.mb, M.nb);
-        const uint8_t* X = M.ws + L.x16 + (size_t)(it.step & 1) * M.mb * M.nb * kOrthoBlk;
+        const OrthoMat& M = p.mat[it.mat];
+        const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
+        const uint8_t* X = M.ws + L.x16 + (it.step & 1) * (L.x32 / 2);
         const uint8_t* S = M.ws + (it.kind == kFull ? L.b16 : L.a16);  // the symmetric operand
-        const int nkb = it.kind == kSym1 ? M.nb : M.mb;
-        const int ra = it.I * 2 + 1 < M.mb ? 2 : 1;
-        const int rb = it.kind == kFull ? (it.J * 2 + 1 < M.nb ? 2 : 1) : (it.J * 2 + 1 < M.mb ? 2 : 1);
-        const bool same = it.kind != kFull && it.I == it.J;  // one operand serves as both
-        for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait(smem_u32(&empty[stage]), phase ^ 1, 3 * lim)) {
-            record_timeout(p.status, abort_flag);
-            break;
-          }
-          const uint32_t bar = smem_u32(&full[stage]);
-          const uint32_t sa = smem_u32(smem + stage * kStageBytes), sb = sa + 2 * kOrthoBlk;
-          mbar_arrive_expect_tx(bar, (uint32_t)((ra + (same ? 0 : rb)) * kOrthoBlk));
-          for (int i = 0; i < ra; ++i) {
-            const int r = it.I * 2 + i;
-            const size_t blk = it.kind == kSym1 ? (size_t)r * M.nb + kb
-                               : (kb >> 1) <= it.I ? (size_t)r * M.mb + kb : (size_t)kb * M.mb + r;
-            bulk_load_1d(sa + i * kOrthoBlk, (it.kind == kSym1 ? X : S) + blk * kOrthoBlk, kOrthoBlk, bar);
-          }
-          if (!same)
-            for (int i = 0; i < rb; ++i) {
-              const int r = it.J * 2 + i;
-              const size_t blk = it.kind == kSym1 ? (size_t)r * M.nb + kb
-                                 : it.kind == kFull ? (size_t)kb * M.nb + r
-                                 : (kb >> 1) <= it.J ? (size_t)r * M.mb + kb : (size_t)kb * M.mb + r;
-              bulk_load_1d(sb + i * kOrthoBlk, (it.kind == kSym2 ? S : X) + blk * kOrthoBlk, kOrthoBlk, bar);
+        const int me = (M.mb + 1) & ~1, ne = (M.nb + 1) & ~1;
+        const int ra = it.I * 4 + (int)rank * 2, rb = it.J * 4 + (int)rank * 2;  // first row of blocks
+        const bool same = it.kind != kFull && it.I == it.J;                      // one operand serves as both
+        const bool la = ra < M.mb, lb = !same && rb < (it.kind == kFull ? M.nb : M.mb);
+        const uint32_t bytes = (uint32_t)((la ? 2 : 0) + (lb ? 2 : 0)) * kOrthoBlk;
+        for (int kb = it.k0; kb < it.k1 && !*abort_flag;) {
+          OperandRun a, b;
+          a.start(it.kind == kGram ? X : S, it.kind == kGram ? ne : me, ra, kb, is_mn(it.kind, false, it.I, kb), la);
+          b.start(it.kind == kSym ? S : X, it.kind == kSym ? me : ne, rb, kb, is_mn(it.kind, true, it.J, kb), lb);
+          for (const int e = run_end(it, kb); kb < e; ++kb) {
+            if (!mbar_wait(smem_u32(&empty[stage]), phase ^ 1, 3 * lim)) {
+              record_timeout(p.status, abort_flag);
+              break;
             }
-          ++issued;
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1;
+            const uint32_t bar = smem_u32(&full[stage]), sa = smem_u32(smem + stage * kStageBytes);
+            mbar_arrive_expect_tx(bar, bytes);
+            a.load(sa, bar, kb);
+            b.load(sa + 2 * kOrthoBlk, bar, kb);
+            ++issued;
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
           }
         }
         if (*abort_flag) break;
@@ -514,205 +636,293 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ O
         }
       }
     }
+    __syncwarp();
   } else if (warp == 1) {
     if (elect_one()) {
       int stage = 0, slot = 0, acc = 0;
       uint32_t phase = 0, rphase = 0, aphase = 0;
       const uint64_t kdesc = smem_desc(0, 16, 1024, 2), mndesc = smem_desc(0, 8192, 1024, 2);
+      const uint32_t far_empty = map_rank(smem_u32(&item_empty[0]), 0);
+      const uint32_t far_full = map_rank(smem_u32(&full[0]), 0);
       while (!*abort_flag) {
-        if (!mbar_wait(smem_u32(&item_full[slot]), rphase, 2 * lim)) {
+        if (!mbar_wait_cluster(smem_u32(&item_full[slot]), rphase, 4 * lim)) {
           record_timeout(p.status, abort_flag);
           break;
         }
         const Item it = ring[slot];
-        mbar_arrive(smem_u32(&item_empty[slot]));
+        mbar_arrive_cluster(far_empty + (uint32_t)slot * 8);
         if (++slot == kRing) {
           slot = 0;
           rphase ^= 1;
         }
         if (it.kind == kStop) break;
-        if (it.kind == kPack) continue;
-        const OrthoMat& M = p.mat[it.mat];
-        const int nkb = it.kind == kSym1 ? M.nb : M.mb;
+        if (rank != 0) {  // tell the leading CTA of each stage that has landed here
+          for (int kb = it.k0; kb < it.k1; ++kb) {
+            if (!mbar_wait(smem_u32(&full[stage]), phase, 4 * lim)) {
+              record_timeout(p.status, abort_flag);
+              break;
+            }
+            mbar_arrive_cluster(far_full + (uint32_t)stage * 8);
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
+          }
+          continue;
+        }
         const bool same = it.kind != kFull && it.I == it.J;
-        if (!mbar_wait(smem_u32(&acc_empty[acc]), aphase ^ 1, 2 * lim)) {
+        if (!mbar_wait_cluster(smem_u32(&acc_empty[acc]), aphase ^ 1, 2 * lim)) {
           record_timeout(p.status, abort_flag);
           break;
         }
         tc_fence_after();
-        const uint32_t d = tmem + (uint32_t)(acc * 128);
-        for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait(smem_u32(&full[stage]), phase, 2 * lim)) {
-            record_timeout(p.status, abort_flag);
-            break;
-          }
-          tc_fence_after();
-          const bool a_mn = it.kind != kSym1 && (kb >> 1) > it.I;
-          const bool b_mn = it.kind == kFull || (it.kind == kSym2 && (kb >> 1) > it.J);
-          const uint32_t sa = desc_addr16(smem_u32(smem + stage * kStageBytes));
-          const uint32_t sb = same ? sa : sa + (2 * kOrthoBlk >> 4);
-          const uint64_t ad = (a_mn ? mndesc : kdesc) + sa, bd = (b_mn ? mndesc : kdesc) + sb;
+        const uint32_t d = tmem + (uint32_t)(acc * 256);
+        for (int kb = it.k0; kb < it.k1 && !*abort_flag;) {
+          const bool a_mn = is_mn(it.kind, false, it.I, kb), b_mn = is_mn(it.kind, true, it.J, kb);
+          const uint64_t ad0 = a_mn ? mndesc : kdesc, bd0 = (b_mn ? mndesc : kdesc) + (same ? 0 : 2 * kOrthoBlk >> 4);
           const uint32_t as = a_mn ? 2048 >> 4 : 32 >> 4, bs = b_mn ? 2048 >> 4 : 32 >> 4;
-          const uint32_t idesc = idesc_f16(128, 128, false, false, true) | (a_mn ? 1u << 15 : 0u) |
+          const uint32_t idesc = idesc_f16(256, 256, false, false, true) | (a_mn ? 1u << 15 : 0u) |
                                  (b_mn ? 1u << 16 : 0u);
+          for (const int e = run_end(it, kb); kb < e; ++kb) {
+            if (!mbar_wait_cluster(smem_u32(&full[stage]), phase, 2 * lim)) {
+              record_timeout(p.status, abort_flag);
+              break;
+            }
+            tc_fence_after();
+            const uint32_t s = desc_addr16(smem_u32(smem + stage * kStageBytes));
+            const uint64_t ad = ad0 + s, bd = bd0 + s;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            tc_mma_f16(d, ad + (uint64_t)(kk * as), bd + (uint64_t)(kk * bs), idesc, kb > 0 || kk > 0);
-          tc_commit(smem_u32(&empty[stage]));
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1;
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_f16_pair(d, ad + (uint64_t)(kk * as), bd + (uint64_t)(kk * bs), idesc, kb > it.k0 || kk > 0);
+            tc_commit_pair(smem_u32(&empty[stage]));
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
           }
         }
         if (*abort_flag) break;
-        tc_commit(smem_u32(&acc_full[acc]));
+        tc_commit_pair(smem_u32(&acc_full[acc]));
         acc ^= 1;
         if (acc == 0) aphase ^= 1;
       }
-      tc_commit(smem_u32(&last));  // nothing runs in TMEM when it is released
-      if (!mbar_wait(smem_u32(&last), 0, lim)) {
-        record_timeout(p.status, abort_flag);
-        drained = 0;
+      if (rank == 0) {  // nothing runs in either CTA's TMEM when it is released
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                         smem_u32(&last))
+                     : "memory");
+        if (!mbar_wait(smem_u32(&last), 0, lim)) {
+          record_timeout(p.status, abort_flag);
+          drained = 0;
+          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_rank(smem_u32(&drained), 1)), "r"(0) : "memory");
+        }
       }
     }
+    __syncwarp();
   } else {
-    const int t = (int)threadIdx.x - 64;
-    const int lane = t & 31, quad = warp & 3;
-    const int row = quad * 32 + lane;     // of the tile (TMEM lane)
-    const int half = t >> 7;              // its columns, 64 of them
+    const int ew = warp - 2, lane = (int)threadIdx.x & 31, quad = warp & 3;
+    const int row = (int)rank * 128 + quad * 32 + lane;  // of the tile
+    const int half = ew >> 2;                            // its columns, 128 of them, 32 at a time
     const int rr = row & 63;
-    int slot = 0, acc = 0, inv_mat = -1;
-    float inv = 0.f;
+    const uint32_t far_item = map_rank(smem_u32(&item_empty[0]), 0), far_acc = map_rank(smem_u32(&acc_empty[0]), 0);
+    const uint32_t stage_w = smem_u32(staging + ew * 4096);  // this warp's 32 rows of a block
+    int slot = 0, acc = 0;
     uint32_t rphase = 0, aphase = 0;
     while (true) {
-      if (!mbar_wait(smem_u32(&item_full[slot]), rphase, 2 * lim)) {
+      if (!mbar_wait_cluster(smem_u32(&item_full[slot]), rphase, 4 * lim)) {
         record_timeout(p.status, abort_flag);
         break;
       }
       const Item it = ring[slot];
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&item_empty[slot]));
+      if (lane == 0) mbar_arrive_cluster(far_item + (uint32_t)slot * 8);
       if (++slot == kRing) {
         slot = 0;
         rphase ^= 1;
       }
       if (it.kind == kStop) break;
       const OrthoMat& M = p.mat[it.mat];
-      if (it.kind == kPack) {
-        pack_block(p, M, it.I, it.J, reinterpret_cast<float*>(staging), red, t, inv_mat, inv, it.mat);
-        fence_proxy_async_all();
-        epi_barrier();
-        if (t == 0) {
-          __threadfence();
-          red_release_add(p.done + it.mat, 1u);
-        }
-        continue;
-      }
-      const OrthoLayout L = ortho_layout(M.mb, M.nb);
+      const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
       const bool full_kind = it.kind == kFull;
       const bool final_step = full_kind && it.step == p.steps - 1;
       const int ncb = full_kind ? M.nb : M.mb;  // block columns of the result
-      const int bi = it.I * 2 + (row >> 6), bj = it.J * 2 + half;
-      const bool in = bi < M.mb && bj < ncb;
-      // what the result adds to the product, loaded while the product runs (the
-      // item's dependency, which the loading warp has seen, covers it)
-      float x[64];
-      float4* x32 = reinterpret_cast<float4*>(M.ws + L.x32 + ((size_t)bi * M.nb + bj) * (2 * kOrthoBlk)) + rr;
-      if (full_kind) {
+      const int bi = it.I * 4 + (row >> 6), bj0 = it.J * 4 + half * 2;
+      const bool any = bi < M.mb && bj0 < ncb;                 // the same in the whole warp
+      const int chunks = !any ? 0 : bj0 + 1 < ncb ? 4 : 2;     // of 32 columns
+      uint8_t* out = M.ws + (it.kind == kGram  ? L.a16
+                             : it.kind == kSym ? L.b16
+                                               : L.x16 + ((it.step + 1) & 1) * (L.x32 / 2));
+      out += ortho_block(bi, bj0, (ncb + 1) & ~1) * kOrthoBlk + (row & 32) * 128;
+      const uint8_t* a16 = M.ws + L.a16 + ortho_block(bi, bj0, (M.mb + 1) & ~1) * kOrthoBlk + rr * 128;
+      float4* x32 = reinterpret_cast<float4*>(M.ws + L.x32 + ((size_t)bi * M.nb + bj0) * (2 * kOrthoBlk)) + rr;
+      const float mul = it.kind == kGram  ? kSa / (kSx * kSx)
+                        : it.kind == kSym ? kC * kSb / (kSa * kSa)
+                                          : 1.f / (kSx * kSb);
+      // what chunk c adds to its product, raw: X, or S in binary16
+      auto load = [&](int c, uint4* v) {
+        if (c >= chunks) return;
+        if (full_kind) {
+          const uint4* s = reinterpret_cast<const uint4*>(x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float4 o = in ? __ldcg(x32 + j * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
-          x[4 * j] = kA * o.x;
-          x[4 * j + 1] = kA * o.y;
-          x[4 * j + 2] = kA * o.z;
-          x[4 * j + 3] = kA * o.w;
+          for (int j = 0; j < 8; ++j) v[j] = __ldcg(s + j * 64);
+        } else if (it.kind == kSym) {
+          const uint8_t* s = a16 + (c >> 1) * (2 * kOrthoBlk);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            v[j] = __ldcg(reinterpret_cast<const uint4*>(s + ((((c & 1) * 4 + j) ^ (rr & 7)) << 4)));
         }
-      } else if (it.kind == kSym2) {
-        const uint8_t* src = M.ws + L.a16 + ((size_t)bi * M.mb + bj) * kOrthoBlk + rr * 128;
+      };
+      // chunk c of the result: the product r, scaled, and v
+      auto store = [&](int c, const uint32_t* r, float scale, const uint4* v) {
+        float x[32];
+        if (full_kind) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint4 o = in ? __ldcg(reinterpret_cast<const uint4*>(src + ((j ^ (rr & 7)) << 4)))
-                             : make_uint4(0, 0, 0, 0);
-          const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+          for (int j = 0; j < 8; ++j) {
+            const float4 o = make_float4(__uint_as_float(v[j].x), __uint_as_float(v[j].y), __uint_as_float(v[j].z),
+                                         __uint_as_float(v[j].w));
+            x[4 * j] = fmaf(kA, o.x, __uint_as_float(r[4 * j]) * scale);
+            x[4 * j + 1] = fmaf(kA, o.y, __uint_as_float(r[4 * j + 1]) * scale);
+            x[4 * j + 2] = fmaf(kA, o.z, __uint_as_float(r[4 * j + 2]) * scale);
+            x[4 * j + 3] = fmaf(kA, o.w, __uint_as_float(r[4 * j + 3]) * scale);
+          }
+          if (final_step) {
+            finish32(p, M, it.I * 256 + row, bj0 * 64 + c * 32, x);
+            return;
+          }
+          float4* s = x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float2 f = h22f(ow[q]);
-            x[8 * j + 2 * q] = f.x * (kB * kSb / kSa);
-            x[8 * j + 2 * q + 1] = f.y * (kB * kSb / kSa);
+          for (int j = 0; j < 8; ++j)
+            __stcg(s + j * 64, make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] *= kSx;
+        } else if (it.kind == kSym) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t h[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float2 f = h22f(h[q]);
+              const int i = 8 * j + 2 * q;
+              x[i] = fmaf(__uint_as_float(r[i]), scale, f.x * (kB * kSb / kSa));
+              x[i + 1] = fmaf(__uint_as_float(r[i + 1]), scale, f.y * (kB * kSb / kSa));
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]) * scale;
+        }
+        if (c == 2) {  // the first block's store has read the staging rows
+          if (lane == 0) bulk_wait_read0();
+          __syncwarp();
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          st_shared_v4(stage_w + (uint32_t)(lane * 128 + ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
+                       make_uint4(f2h2(x[8 * h], x[8 * h + 1]), f2h2(x[8 * h + 2], x[8 * h + 3]),
+                                  f2h2(x[8 * h + 4], x[8 * h + 5]), f2h2(x[8 * h + 6], x[8 * h + 7])));
+        if (c & 1) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            bulk_store_1d(out + (c >> 1) * (2 * kOrthoBlk), stage_w, 4096);
+            bulk_commit();
           }
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 64; ++j) x[j] = 0.f;
-      }
-      if (!mbar_wait(smem_u32(&acc_full[acc]), aphase, 2 * lim)) {
+      };
+      uint4 va[8], vb[8];
+      load(0, va);  // (the item's dependency, which the loading warp has seen, covers these)
+      if (!mbar_wait_cluster(smem_u32(&acc_full[acc]), aphase, 4 * lim)) {
         record_timeout(p.status, abort_flag);
         break;
       }
       tc_fence_after();
-      const float mul = it.kind == kSym1   ? kSa / (kSx * kSx)
-                        : it.kind == kSym2 ? kC * kSb / (kSa * kSa)
-                                           : 1.f / (kSx * kSb);
-#pragma unroll
-      for (int c = 0; c < 64; c += 32) {
-        uint32_t r[32];
-        tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 128 + half * 64 + c), r);
-        tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 128 + half * 64 + c + 16), r + 16);
+      const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * 128);
+      auto product = [&](int c, uint32_t* r) {
+        tmem_ld16(tacc + (uint32_t)(c * 32), r);
+        tmem_ld16(tacc + (uint32_t)(c * 32 + 16), r + 16);
         tmem_ld_wait();
+      };
+      bool signal = any || it.split == 0;
+      if (it.kind == kGram && M.splits > 1) {
+        if (any) {
+          // this part of the sum; the last part to arrive adds them all, in order
+          const int slice = (ortho_sym(it.I) + it.J) * kOrthoSignals + (int)rank * 8 + ew;
+          float4* part = reinterpret_cast<float4*>(
+                             M.ws + L.part +
+                             ((size_t)(ortho_sym(it.I) + it.J) * M.splits * kOrthoSignals + rank * 8 + ew) *
+                                 kOrthoPart) + lane;
+          constexpr int kNext = kOrthoSignals * kOrthoPart / 16;  // float4s to the next part
+#pragma unroll 1
+          for (int c = 0; c < chunks; ++c) {
+            uint32_t r[32];
+            product(c, r);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[c + j] = fmaf(__uint_as_float(r[j]), mul, x[c + j]);
-      }
-      if (final_step) {
-        if (in) finish64(p, M, it.I * 128 + row, it.J * 128 + half * 64, x);
-      } else {
-        if (full_kind) {
-          if (in) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              __stcg(x32 + j * 64, make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
+            for (int j = 0; j < 8; ++j)
+              __stcg(part + it.split * kNext + (c * 8 + j) * 32,
+                     make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]),
+                                 __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3])));
           }
+          uint32_t seen = 0;
+          __syncwarp();
+          if (lane == 0) {
+            __threadfence();
+            seen = atomicAdd(M.arrivals + slice, 1u);
+            __threadfence();
+          }
+          seen = __shfl_sync(0xffffffffu, seen, 0);
+          __syncwarp();
+          signal = seen % (uint32_t)M.splits == (uint32_t)M.splits - 1;
+          if (signal) {
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+              float x[32];
 #pragma unroll
-          for (int j = 0; j < 64; ++j) x[j] *= kSx;
+              for (int j = 0; j < 32; ++j) x[j] = 0.f;
+#pragma unroll 2
+              for (int s = 0; s < M.splits; ++s) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const float4 o = __ldcg(part + s * kNext + (c * 8 + j) * 32);
+                  x[4 * j] += o.x;
+                  x[4 * j + 1] += o.y;
+                  x[4 * j + 2] += o.z;
+                  x[4 * j + 3] += o.w;
+                }
+              }
+              store(c, reinterpret_cast<const uint32_t*>(x), mul, va);
+            }
+          }
         }
-        const uint32_t st = smem_u32(staging) + (uint32_t)(((row >> 6) * 2 + half) * kOrthoBlk + rr * 128);
-#pragma unroll
-        for (int h = 0; h < 8; ++h)
-          st_shared_v4(st + (uint32_t)((h ^ (rr & 7)) << 4),
-                       make_uint4(f2h2(x[8 * h], x[8 * h + 1]), f2h2(x[8 * h + 2], x[8 * h + 3]),
-                                  f2h2(x[8 * h + 4], x[8 * h + 5]), f2h2(x[8 * h + 6], x[8 * h + 7])));
+      } else {
+        for (int c = 0; c < chunks; c += 2) {
+          uint32_t r[32];
+          load(c + 1, vb);
+          product(c, r);
+          store(c, r, mul, va);
+          load(c + 2, va);
+          product(c + 1, r);
+          store(c + 1, r, mul, vb);
+        }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
+      if (lane == 0) {
+        mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
+        if (signal) {
+          bulk_wait0();
+          red_release_add(p.done + it.mat, 1u);
+        }
+      }
+      __syncwarp();
       acc ^= 1;
       if (acc == 0) aphase ^= 1;
-      fence_proxy_async_all();
-      epi_barrier();
-      if (t == 0) {
-        if (!final_step) {
-          uint8_t* out = M.ws + (it.kind == kSym1   ? L.a16
-                                 : it.kind == kSym2 ? L.b16
-                                                    : L.x16 + (size_t)((it.step + 1) & 1) * M.mb * M.nb * kOrthoBlk);
-          for (int q = 0; q < 4; ++q) {
-            const int obi = it.I * 2 + (q >> 1), obj = it.J * 2 + (q & 1);
-            if (obi < M.mb && obj < ncb)
-              bulk_store_1d(out + ((size_t)obi * ncb + obj) * kOrthoBlk, smem_u32(staging) + q * kOrthoBlk, kOrthoBlk);
-          }
-          bulk_commit();
-          bulk_wait0();
-          fence_proxy_async_all();
-        }
-        __threadfence();
-        red_release_add(p.done + it.mat, 1u);
-      }
-      epi_barrier();  // the staging buffer is free again
     }
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync();  // neither CTA leaves while the other may still reach into it
   if (warp == 1 && drained) {
     tc_fence_after();
-    tmem_dealloc(tmem, 256);
+    tmem_dealloc_pair(tmem, 512);
   }
 }
 
@@ -721,10 +931,12 @@ cudaError_t launch_ortho(const OrthoParams& p, int sms, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(k_ortho_norm, dim3((unsigned)p.total_parts), dim3(256), 0, s, p);
   if (e != cudaSuccess) return e;
-  const int grid = p.max_items < sms ? p.max_items : sms;
-  e = launch_pdl(k_ortho, dim3((unsigned)grid), dim3(kThreads), kOrthoSmem, s, p);
+  e = launch_pdl(k_ortho_pack, dim3((unsigned)p.pre_pack[p.count]), dim3(256), 0, s, p);
   if (e != cudaSuccess) return e;
-  return counted_launches(2);
+  const int pairs = p.max_items < sms / 2 ? p.max_items : sms / 2;
+  e = launch_pdl(k_ortho, dim3((unsigned)(2 * pairs)), dim3(kThreads), kOrthoSmem, s, p);
+  if (e != cudaSuccess) return e;
+  return counted_launches(3);
 }
 
 }  // namespace pf16

@@ -10,48 +10,73 @@ constexpr int kOrthoMaxParts = 512;  // partial sums of squares of one matrix
 constexpr int kOrthoBlk = 8192;      // bytes of a 64 x 64 binary16 block
 
 // One matrix.  Inside, it is m x n with m <= n (transposed when `tall`), kept as
-// a grid of mb x nb blocks of 64 x 64 elements, zero past its edges.
+// a grid of mb x nb blocks of 64 x 64 elements, zero past its edges.  Binary16 blocks of two
+// neighbouring rows of blocks alternate (ortho_block), so that 128 rows of an operand are one
+// contiguous copy; their grids are allocated for even sizes, and what lies in the odd block past
+// an edge is multiplied into rows or columns of a tile that nobody stores.
 struct OrthoMat {
   const uint16_t* g;
   uint16_t* v;        // momentum (null: plain orthogonalisation)
   uint16_t* w;        // weights updated in place, or the output
-  uint8_t* ws;        // x16[2], x32, a16, b16 (ortho_layout)
+  uint8_t* ws;        // x16[2], x32, a16, b16, split sums (ortho_layout)
+  uint32_t* arrivals; // of the split sums
   int rows, cols;     // as the caller sees it
   int mb, nb;
   int part0, parts;   // its partial sums of squares
   int tall;
+  int splits, kper;   // X X^T: parts of the sum over n, and blocks of n in each
   float scale;        // of the orthogonalised update in the weights' step
 };
 
 struct OrthoParams {
   int count, steps;
   int max_items;      // most work items of one phase, over all matrices together
+  size_t zero_words;  // counters, from `ticket` on
   int muon, nesterov;
   float lr, momentum, wd;
   uint32_t* ticket;   // work items handed out
-  uint32_t* done;     // [count] items finished of each matrix
+  uint32_t* done;     // [count] parts of items finished of each matrix (kOrthoSignals an item)
   float* parts;       // partial sums of squares
   int total_parts;
   int* status;
   unsigned long long wait_limit_ns;
-  // first item of each matrix within each kind of phase (pack, symmetric
-  // product, full product); entry `count` is the kind's total
-  int pre_pack[kOrthoMax + 1], pre_sym[kOrthoMax + 1], pre_full[kOrthoMax + 1];
+  int pre_pack[kOrthoMax + 1];  // first block of each matrix, and their number
+  // first item of each matrix within each kind of phase (X X^T, the
+  // symmetric product of S, the full product); entry `count` is the kind's total
+  int pre_gram[kOrthoMax + 1], pre_sym[kOrthoMax + 1], pre_full[kOrthoMax + 1];
   OrthoMat mat[kOrthoMax];
 };
 
+// Tiles of a product are 256 x 256, made by a pair of CTAs; each of the pair's
+// 2 x 8 epilogue warps signals its part of an item.
+constexpr int kOrthoSignals = 16;
+constexpr int kOrthoPairs = 76;      // of SMs
+__host__ __device__ inline int ortho_tiles(int blocks) { return (blocks + 3) >> 2; }
+__host__ __device__ inline int ortho_sym(int tiles) { return tiles * (tiles + 1) / 2; }
+
+// Split sums of X X^T: FP32 parts [tile][split][CTA of the pair][warp], 16 KB each, and an
+// arrival counter for each [tile][CTA of the pair][warp].
+constexpr int kOrthoPart = 16384;
+
 struct OrthoLayout {
-  size_t x16, x32, a16, b16, bytes;
+  size_t x16, x32, a16, b16, part, bytes;
 };
-__host__ __device__ inline OrthoLayout ortho_layout(long long mb, long long nb) {
+__host__ __device__ inline OrthoLayout ortho_layout(long long mb, long long nb, int splits) {
   OrthoLayout l;
-  const size_t xb = (size_t)mb * nb * kOrthoBlk, ab = (size_t)mb * mb * kOrthoBlk;
-  l.x16 = 0;            // two buffers of xb bytes
+  const size_t me = (mb + 1) & ~1ll, ne = (nb + 1) & ~1ll;
+  const size_t xb = me * ne * kOrthoBlk, ab = me * me * kOrthoBlk;
+  l.x16 = 0;  // two buffers of xb bytes
   l.x32 = 2 * xb;
-  l.a16 = 4 * xb;
-  l.b16 = 4 * xb + ab;
-  l.bytes = 4 * xb + 2 * ab;
+  l.a16 = l.x32 + (size_t)mb * nb * (2 * kOrthoBlk);
+  l.b16 = l.a16 + ab;
+  l.part = l.b16 + ab;
+  l.bytes = l.part + (splits > 1 ? (size_t)ortho_sym(ortho_tiles((int)mb)) * splits * kOrthoSignals * kOrthoPart : 0);
   return l;
+}
+
+// Index of block (i, j) in a binary16 grid of `cols` (even) block columns.
+__host__ __device__ inline size_t ortho_block(int i, int j, int cols) {
+  return ((size_t)(i >> 1) * cols + j) * 2 + (i & 1);
 }
 
 cudaError_t launch_ortho(const OrthoParams& p, int sms, cudaStream_t s);
