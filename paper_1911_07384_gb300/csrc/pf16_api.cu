@@ -1675,6 +1675,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     return la != lb ? la > lb : a < b;
   });
   p->count = count;
+  p->ws = base;
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
   size_t words = 4 + (size_t)count;
@@ -1813,7 +1814,9 @@ static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int3
   int sms;
   rc = device_consts(&p.status, &sms);
   if (rc != PF16_OK) return rc;
-  return launch_ortho(p, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK : PF16_ERR_CUDA;
+  CUtensorMap map;
+  if (!driver_fns() || !map_2d(&map, ws, 64, need / 128, 64, 64, 64, CU_TENSOR_MAP_SWIZZLE_NONE)) return PF16_ERR_CUDA;
+  return launch_ortho(p, map, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK : PF16_ERR_CUDA;
 }
 
 size_t pf16_ortho_workspace_size(const pf16_ortho_matrix* mats, int32_t count) { return ortho_ws(mats, nullptr, count); }

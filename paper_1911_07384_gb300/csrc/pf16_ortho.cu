@@ -445,14 +445,17 @@ __device__ __forceinline__ void finish32(const OrthoParams& p, const OrthoMat& M
   const long long pitch = M.tall ? M.cols : 1;
   uint16_t* o = M.tall ? M.w + (long long)c * M.cols + r : M.w + (long long)r * M.cols + c;
   const int left = (M.tall ? M.rows : M.cols) - c;
-  float w[32];
-  if (p.muon) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) w[j] = j < left ? h2f(o[j * pitch]) : 0.f;
+  for (int h = 0; h < 32; h += 8) {
+    float w[8];
+    if (p.muon) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = h + j < left ? h2f(o[(h + j) * pitch]) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (h + j < left) o[(h + j) * pitch] = f2h(p.muon ? muon_w(p, M, w[j], x[h + j]) : x[h + j]);
   }
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < left) o[j * pitch] = f2h(p.muon ? muon_w(p, M, w[j], x[j]) : x[j]);
 }
 
 __device__ __forceinline__ void record_timeout(int* status, volatile int* abort_flag) {
@@ -480,40 +483,138 @@ __device__ __forceinline__ int run_end(const Item& it, int kb) {
   return e;
 }
 
-// 128 rows of an operand, block after block along the sum: one copy of 16 KB, or, transposed,
-// two of 8 KB.
+// One 8 KB block of the workspace, which `map` describes as rows of 128 bytes, signalling the leading
+// CTA's barrier.
+__device__ __forceinline__ void load_block(const CUtensorMap* map, uint32_t dst, uint32_t bar, int row) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(row)
+      : "memory");
+}
+
+// 128 rows of an operand, two blocks, for block after block along the sum.  Positions count rows of
+// 128 bytes in the workspace, 64 a block.
 struct OperandRun {
-  const uint8_t* at;
-  size_t even, odd;  // to the next block from an even one, from an odd one
-  bool mn, live;
-  __device__ __forceinline__ void start(const uint8_t* grid, int pitch, int row, int kb, bool mn_, bool live_) {
-    mn = mn_;
+  int at, second, even, odd;  // to the second block; to the next ones from an even block, from an odd one
+  bool live;
+  __device__ __forceinline__ void start(int grid, int pitch, int row, int kb, bool mn, bool live_) {
     live = live_;
-    at = grid + (mn ? ortho_block(kb, row, pitch) : ortho_block(row, kb, pitch)) * kOrthoBlk;
-    even = mn ? kOrthoBlk : 2 * kOrthoBlk;
-    odd = mn ? (size_t)(2 * pitch - 1) * kOrthoBlk : 2 * kOrthoBlk;
+    at = grid + 64 * (int)(mn ? ortho_block(kb, row, pitch) : ortho_block(row, kb, pitch));
+    second = mn ? 128 : 64;
+    even = mn ? 64 : 128;
+    odd = mn ? 64 * (2 * pitch - 1) : 128;
   }
-  __device__ __forceinline__ void load(uint32_t dst, uint32_t bar, int kb) {
+  __device__ __forceinline__ void load(const CUtensorMap* map, uint32_t dst, uint32_t bar, int kb) {
     if (live) {
-      if (mn) {
-        bulk_load_1d(dst, at, kOrthoBlk, bar);
-        bulk_load_1d(dst + kOrthoBlk, at + 2 * kOrthoBlk, kOrthoBlk, bar);
-      } else {
-        bulk_load_1d(dst, at, 2 * kOrthoBlk, bar);
-      }
+      load_block(map, dst, bar, at);
+      load_block(map, dst + kOrthoBlk, bar, at + second);
     }
     at += (kb & 1) ? odd : even;
   }
 };
 
+// One epilogue warp's part of a tile: 32 rows, 128 columns in chunks of 32.
+struct TileOut {
+  const OrthoParams& p;
+  const OrthoMat& M;
+  const Item& it;
+  uint8_t* out;         // the binary16 result: this warp's rows of its first block
+  const uint8_t* a16;   // S there: this lane's row
+  float4* x32;          // X there
+  float mul;            // of the product
+  uint32_t stage_w;
+  int chunks, rr, lane, row, bj0;
+  bool full_kind, final_step;
+
+  // what chunk c adds to its product, raw: X, or S in binary16
+  __device__ __forceinline__ void load(int c, uint4* v) const {
+    if (c >= chunks) return;
+    if (full_kind) {
+      const uint4* s = reinterpret_cast<const uint4*>(x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __ldcg(s + j * 64);
+    } else if (it.kind == kSym) {
+      const uint8_t* s = a16 + (c >> 1) * (2 * kOrthoBlk);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = __ldcg(reinterpret_cast<const uint4*>(s + ((((c & 1) * 4 + j) ^ (rr & 7)) << 4)));
+    }
+  }
+
+  // chunk c of the result: the product x, scaled, and v
+  __device__ __forceinline__ void store(int c, uint32_t* x, const uint4* v) const {
+    if (full_kind) {
+      float4* s = x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t old[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        float y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          y[q] = fmaf(kA, __uint_as_float(old[q]), __uint_as_float(x[4 * j + q]) * mul);
+        if (!final_step) __stcg(s + j * 64, make_float4(y[0], y[1], y[2], y[3]));
+        const float copy = final_step ? 1.f : kSx;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[4 * j + q] = __float_as_uint(y[q] * copy);
+      }
+      if (final_step) {
+        finish32(p, M, it.I * 256 + row, bj0 * 64 + c * 32, reinterpret_cast<const float*>(x));
+        return;
+      }
+    } else if (it.kind == kSym) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t h[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 f = h22f(h[q]);
+          const int i = 8 * j + 2 * q;
+          x[i] = __float_as_uint(fmaf(__uint_as_float(x[i]), mul, f.x * (kB * kSb / kSa)));
+          x[i + 1] = __float_as_uint(fmaf(__uint_as_float(x[i + 1]), mul, f.y * (kB * kSb / kSa)));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * mul);
+    }
+    if (c == 2) {  // the first block's store has read the staging rows
+      if (lane == 0) bulk_wait_read0();
+      __syncwarp();
+    }
+    const float* f = reinterpret_cast<const float*>(x);
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      st_shared_v4(stage_w + (uint32_t)(lane * 128 + ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
+                   make_uint4(f2h2(f[8 * h], f[8 * h + 1]), f2h2(f[8 * h + 2], f[8 * h + 3]),
+                              f2h2(f[8 * h + 4], f[8 * h + 5]), f2h2(f[8 * h + 6], f[8 * h + 7])));
+    if (c & 1) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        bulk_store_1d(out + (c >> 1) * (2 * kOrthoBlk), stage_w, 4096);
+        bulk_commit();
+      }
+    }
+  }
+};
+
+// 32 columns of this warp's 32 accumulator rows
+__device__ __forceinline__ void product(uint32_t tacc, int c, uint32_t* r) {
+  tmem_ld16(tacc + (uint32_t)(c * 32), r);
+  tmem_ld16(tacc + (uint32_t)(c * 32 + 16), r + 16);
+  tmem_ld_wait();
+}
+
 }  // namespace
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho(const __grid_constant__ OrthoParams p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    k_ortho(const __grid_constant__ OrthoParams p, const __grid_constant__ CUtensorMap map) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* staging = smem + kStages * kStageBytes;
-  // (item_empty and acc_empty are used in the leading CTA only)
+  // (full, item_empty and acc_empty are used in the leading CTA only)
   __shared__ uint64_t full[kStages], empty[kStages], item_full[kRing], item_empty[kRing], acc_full[2], acc_empty[2],
       last;
   __shared__ Item ring[kRing];
@@ -524,12 +625,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_u32(&full[i]), rank == 0 ? 2 : 1);  // the leading CTA's: both CTAs' operands
+      mbar_init(smem_u32(&full[i]), 2);  // the leading CTA's: both CTAs' copies and loading warps
       mbar_init(smem_u32(&empty[i]), 1);
     }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&item_full[i]), 1);
-      mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32 + 2 + kEpi / 32);  // every reader in both CTAs
+      mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32 + 1 + kEpi / 32);  // every reader in both CTAs
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&acc_full[i]), 1);
@@ -553,6 +654,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
     if (elect_one()) {
       int stage = 0, slot = 0;
       uint32_t phase = 0, rphase = 0, issued = 0;
+      const uint32_t far_full = map_rank(smem_u32(&full[0]), 0);
       uint32_t ticket = rank == 0 ? atomicAdd(p.ticket, 1u) : 0;
       while (true) {
         Item it;
@@ -599,13 +701,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
         fence_proxy_async_all();  // the blocks' writers used both proxies
         const OrthoMat& M = p.mat[it.mat];
         const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
-        const uint8_t* X = M.ws + L.x16 + (it.step & 1) * (L.x32 / 2);
-        const uint8_t* S = M.ws + (it.kind == kFull ? L.b16 : L.a16);  // the symmetric operand
+        const int base = (int)((M.ws - p.ws) >> 7);
+        const int X = base + (int)((L.x16 + (it.step & 1) * (L.x32 / 2)) >> 7);
+        const int S = base + (int)((it.kind == kFull ? L.b16 : L.a16) >> 7);  // the symmetric operand
         const int me = (M.mb + 1) & ~1, ne = (M.nb + 1) & ~1;
         const int ra = it.I * 4 + (int)rank * 2, rb = it.J * 4 + (int)rank * 2;  // first row of blocks
         const bool same = it.kind != kFull && it.I == it.J;                      // one operand serves as both
-        const bool la = ra < M.mb, lb = !same && rb < (it.kind == kFull ? M.nb : M.mb);
-        const uint32_t bytes = (uint32_t)((la ? 2 : 0) + (lb ? 2 : 0)) * kOrthoBlk;
+        const int rows_b = it.kind == kFull ? M.nb : M.mb;
+        const bool la = ra < M.mb, lb = !same && rb < rows_b;
+        // both CTAs' bytes (the first rows of a tile, the leading CTA's, are never past the edge)
+        const uint32_t bytes = 2 * kOrthoBlk * (uint32_t)(1 + (it.I * 4 + 2 < M.mb ? 1 : 0) +
+                                                          (same ? 0 : 1 + (it.J * 4 + 2 < rows_b ? 1 : 0)));
         for (int kb = it.k0; kb < it.k1 && !*abort_flag;) {
           OperandRun a, b;
           a.start(it.kind == kGram ? X : S, it.kind == kGram ? ne : me, ra, kb, is_mn(it.kind, false, it.I, kb), la);
@@ -615,10 +721,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
               record_timeout(p.status, abort_flag);
               break;
             }
-            const uint32_t bar = smem_u32(&full[stage]), sa = smem_u32(smem + stage * kStageBytes);
-            mbar_arrive_expect_tx(bar, bytes);
-            a.load(sa, bar, kb);
-            b.load(sa + 2 * kOrthoBlk, bar, kb);
+            const uint32_t bar = far_full + (uint32_t)stage * 8, sa = smem_u32(smem + stage * kStageBytes);
+            // The other CTA arrives for every stage, also where it has nothing to load: the leading
+            // one must not get ahead of it, whose `empty` would pass a phase that it never saw.
+            if (rank == 0)
+              mbar_arrive_expect_tx(smem_u32(&full[stage]), bytes);
+            else
+              mbar_arrive_cluster(bar);
+            a.load(&map, sa, bar, kb);
+            b.load(&map, sa + 2 * kOrthoBlk, bar, kb);
             ++issued;
             if (++stage == kStages) {
               stage = 0;
@@ -628,7 +739,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
         }
         if (*abort_flag) break;
       }
-      if (*abort_flag) {  // copies in flight land before the CTA ends
+      // copies in flight land before the CTA ends: the leading CTA's barriers count both CTAs', and
+      // neither CTA ends before the other
+      if (rank == 0 && *abort_flag) {
         for (int i = 0; i < kStages && (uint32_t)i < issued; ++i) {
           stage = stage == 0 ? kStages - 1 : stage - 1;
           if (stage == kStages - 1) phase ^= 1;
@@ -638,38 +751,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (elect_one()) {
+    if (rank == 0 && elect_one()) {
       int stage = 0, slot = 0, acc = 0;
       uint32_t phase = 0, rphase = 0, aphase = 0;
       const uint64_t kdesc = smem_desc(0, 16, 1024, 2), mndesc = smem_desc(0, 8192, 1024, 2);
-      const uint32_t far_empty = map_rank(smem_u32(&item_empty[0]), 0);
-      const uint32_t far_full = map_rank(smem_u32(&full[0]), 0);
       while (!*abort_flag) {
         if (!mbar_wait_cluster(smem_u32(&item_full[slot]), rphase, 4 * lim)) {
           record_timeout(p.status, abort_flag);
           break;
         }
         const Item it = ring[slot];
-        mbar_arrive_cluster(far_empty + (uint32_t)slot * 8);
+        mbar_arrive(smem_u32(&item_empty[slot]));
         if (++slot == kRing) {
           slot = 0;
           rphase ^= 1;
         }
         if (it.kind == kStop) break;
-        if (rank != 0) {  // tell the leading CTA of each stage that has landed here
-          for (int kb = it.k0; kb < it.k1; ++kb) {
-            if (!mbar_wait(smem_u32(&full[stage]), phase, 4 * lim)) {
-              record_timeout(p.status, abort_flag);
-              break;
-            }
-            mbar_arrive_cluster(far_full + (uint32_t)stage * 8);
-            if (++stage == kStages) {
-              stage = 0;
-              phase ^= 1;
-            }
-          }
-          continue;
-        }
         const bool same = it.kind != kFull && it.I == it.J;
         if (!mbar_wait_cluster(smem_u32(&acc_empty[acc]), aphase ^ 1, 2 * lim)) {
           record_timeout(p.status, abort_flag);
@@ -706,15 +803,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
         acc ^= 1;
         if (acc == 0) aphase ^= 1;
       }
-      if (rank == 0) {  // nothing runs in either CTA's TMEM when it is released
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                         smem_u32(&last))
-                     : "memory");
-        if (!mbar_wait(smem_u32(&last), 0, lim)) {
-          record_timeout(p.status, abort_flag);
-          drained = 0;
-          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_rank(smem_u32(&drained), 1)), "r"(0) : "memory");
-        }
+      // nothing runs in either CTA's TMEM when it is released
+      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&last))
+                   : "memory");
+      if (!mbar_wait(smem_u32(&last), 0, lim)) {
+        record_timeout(p.status, abort_flag);
+        drained = 0;
+        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_rank(smem_u32(&drained), 1)), "r"(0) : "memory");
       }
     }
     __syncwarp();
@@ -757,90 +852,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
       const float mul = it.kind == kGram  ? kSa / (kSx * kSx)
                         : it.kind == kSym ? kC * kSb / (kSa * kSa)
                                           : 1.f / (kSx * kSb);
-      // what chunk c adds to its product, raw: X, or S in binary16
-      auto load = [&](int c, uint4* v) {
-        if (c >= chunks) return;
-        if (full_kind) {
-          const uint4* s = reinterpret_cast<const uint4*>(x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __ldcg(s + j * 64);
-        } else if (it.kind == kSym) {
-          const uint8_t* s = a16 + (c >> 1) * (2 * kOrthoBlk);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] = __ldcg(reinterpret_cast<const uint4*>(s + ((((c & 1) * 4 + j) ^ (rr & 7)) << 4)));
-        }
-      };
-      // chunk c of the result: the product r, scaled, and v
-      auto store = [&](int c, const uint32_t* r, float scale, const uint4* v) {
-        float x[32];
-        if (full_kind) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float4 o = make_float4(__uint_as_float(v[j].x), __uint_as_float(v[j].y), __uint_as_float(v[j].z),
-                                         __uint_as_float(v[j].w));
-            x[4 * j] = fmaf(kA, o.x, __uint_as_float(r[4 * j]) * scale);
-            x[4 * j + 1] = fmaf(kA, o.y, __uint_as_float(r[4 * j + 1]) * scale);
-            x[4 * j + 2] = fmaf(kA, o.z, __uint_as_float(r[4 * j + 2]) * scale);
-            x[4 * j + 3] = fmaf(kA, o.w, __uint_as_float(r[4 * j + 3]) * scale);
-          }
-          if (final_step) {
-            finish32(p, M, it.I * 256 + row, bj0 * 64 + c * 32, x);
-            return;
-          }
-          float4* s = x32 + (c >> 1) * (2 * kOrthoBlk / 16) + (c & 1) * 8 * 64;
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            __stcg(s + j * 64, make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
-#pragma unroll
-          for (int j = 0; j < 32; ++j) x[j] *= kSx;
-        } else if (it.kind == kSym) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t h[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float2 f = h22f(h[q]);
-              const int i = 8 * j + 2 * q;
-              x[i] = fmaf(__uint_as_float(r[i]), scale, f.x * (kB * kSb / kSa));
-              x[i + 1] = fmaf(__uint_as_float(r[i + 1]), scale, f.y * (kB * kSb / kSa));
-            }
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]) * scale;
-        }
-        if (c == 2) {  // the first block's store has read the staging rows
-          if (lane == 0) bulk_wait_read0();
-          __syncwarp();
-        }
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-          st_shared_v4(stage_w + (uint32_t)(lane * 128 + ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
-                       make_uint4(f2h2(x[8 * h], x[8 * h + 1]), f2h2(x[8 * h + 2], x[8 * h + 3]),
-                                  f2h2(x[8 * h + 4], x[8 * h + 5]), f2h2(x[8 * h + 6], x[8 * h + 7])));
-        if (c & 1) {
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            bulk_store_1d(out + (c >> 1) * (2 * kOrthoBlk), stage_w, 4096);
-            bulk_commit();
-          }
-        }
-      };
+      const TileOut o{p, M, it, out, a16, x32, mul, stage_w, chunks, rr, lane, row, bj0, full_kind, final_step};
+      // two chunks' addends are loaded while the product runs (the item's dependency, which the
+      // loading warp has seen, covers them), the others' as registers come free
       uint4 va[8], vb[8];
-      load(0, va);  // (the item's dependency, which the loading warp has seen, covers these)
+      o.load(0, va);
+      o.load(1, vb);
       if (!mbar_wait_cluster(smem_u32(&acc_full[acc]), aphase, 4 * lim)) {
         record_timeout(p.status, abort_flag);
         break;
       }
       tc_fence_after();
       const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * 128);
-      auto product = [&](int c, uint32_t* r) {
-        tmem_ld16(tacc + (uint32_t)(c * 32), r);
-        tmem_ld16(tacc + (uint32_t)(c * 32 + 16), r + 16);
-        tmem_ld_wait();
-      };
       bool signal = any || it.split == 0;
       if (it.kind == kGram && M.splits > 1) {
         if (any) {
@@ -854,7 +877,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
 #pragma unroll 1
           for (int c = 0; c < chunks; ++c) {
             uint32_t r[32];
-            product(c, r);
+            product(tacc, c, r);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               __stcg(part + it.split * kNext + (c * 8 + j) * 32,
@@ -874,33 +897,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
           if (signal) {
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
-              float x[32];
+              uint32_t x[32];
 #pragma unroll
-              for (int j = 0; j < 32; ++j) x[j] = 0.f;
-#pragma unroll 2
+              for (int j = 0; j < 32; ++j) x[j] = 0;
+#pragma unroll 3
               for (int s = 0; s < M.splits; ++s) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                  const float4 o = __ldcg(part + s * kNext + (c * 8 + j) * 32);
-                  x[4 * j] += o.x;
-                  x[4 * j + 1] += o.y;
-                  x[4 * j + 2] += o.z;
-                  x[4 * j + 3] += o.w;
+                  const float4 f = __ldcg(part + s * kNext + (c * 8 + j) * 32);
+                  x[4 * j] = __float_as_uint(__uint_as_float(x[4 * j]) + f.x);
+                  x[4 * j + 1] = __float_as_uint(__uint_as_float(x[4 * j + 1]) + f.y);
+                  x[4 * j + 2] = __float_as_uint(__uint_as_float(x[4 * j + 2]) + f.z);
+                  x[4 * j + 3] = __float_as_uint(__uint_as_float(x[4 * j + 3]) + f.w);
                 }
               }
-              store(c, reinterpret_cast<const uint32_t*>(x), mul, va);
+              o.store(c, x, va);
             }
           }
         }
       } else {
-        for (int c = 0; c < chunks; c += 2) {
-          uint32_t r[32];
-          load(c + 1, vb);
-          product(c, r);
-          store(c, r, mul, va);
-          load(c + 2, va);
-          product(c + 1, r);
-          store(c + 1, r, mul, vb);
+        uint32_t r[32];
+        if (chunks > 0) {
+          product(tacc, 0, r);
+          o.store(0, r, va);
+          o.load(2, va);
+          product(tacc, 1, r);
+          o.store(1, r, vb);
+          o.load(3, vb);
+        }
+        if (chunks > 2) {
+          product(tacc, 2, r);
+          o.store(2, r, va);
+          product(tacc, 3, r);
+          o.store(3, r, vb);
         }
       }
       tc_fence_before();
@@ -926,7 +955,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ortho
   }
 }
 
-cudaError_t launch_ortho(const OrthoParams& p, int sms, cudaStream_t s) {
+cudaError_t launch_ortho(const OrthoParams& p, const CUtensorMap& map, int sms, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(k_ortho, cudaFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmem);
   if (e != cudaSuccess) return e;
   e = launch_pdl(k_ortho_norm, dim3((unsigned)p.total_parts), dim3(256), 0, s, p);
@@ -934,7 +963,7 @@ cudaError_t launch_ortho(const OrthoParams& p, int sms, cudaStream_t s) {
   e = launch_pdl(k_ortho_pack, dim3((unsigned)p.pre_pack[p.count]), dim3(256), 0, s, p);
   if (e != cudaSuccess) return e;
   const int pairs = p.max_items < sms / 2 ? p.max_items : sms / 2;
-  e = launch_pdl(k_ortho, dim3((unsigned)(2 * pairs)), dim3(kThreads), kOrthoSmem, s, p);
+  e = launch_pdl(k_ortho, dim3((unsigned)(2 * pairs)), dim3(kThreads), kOrthoSmem, s, p, map);
   if (e != cudaSuccess) return e;
   return counted_launches(3);
 }

@@ -1,6 +1,7 @@
 // Orthogonalised updates (pf16_ortho.cu): what the C-ABI layer hands to the kernels.
 #pragma once
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 namespace pf16 {
@@ -34,6 +35,7 @@ struct OrthoParams {
   size_t zero_words;  // counters, from `ticket` on
   int muon, nesterov;
   float lr, momentum, wd;
+  const uint8_t* ws;  // what the tensor map describes: every matrix's buffers lie a multiple of 128 bytes in
   uint32_t* ticket;   // work items handed out
   uint32_t* done;     // [count] parts of items finished of each matrix (kOrthoSignals an item)
   float* parts;       // partial sums of squares
@@ -79,6 +81,7 @@ __host__ __device__ inline size_t ortho_block(int i, int j, int cols) {
   return ((size_t)(i >> 1) * cols + j) * 2 + (i & 1);
 }
 
-cudaError_t launch_ortho(const OrthoParams& p, int sms, cudaStream_t s);
+// map: the workspace as rows of 128 bytes, boxes of 64 of them, not swizzled.
+cudaError_t launch_ortho(const OrthoParams& p, const CUtensorMap& map, int sms, cudaStream_t s);
 
 }  // namespace pf16
