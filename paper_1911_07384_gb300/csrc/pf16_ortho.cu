@@ -180,6 +180,9 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t saddr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t mapped) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t mapped) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
+}
 __device__ __forceinline__ void st_cluster_v4(uint32_t mapped, int a, int b, int c, int d) {
   asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mapped), "r"(a), "r"(b), "r"(c), "r"(d)
                : "memory");
@@ -724,10 +727,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const uint32_t bar = far_full + (uint32_t)stage * 8, sa = smem_u32(smem + stage * kStageBytes);
             // The other CTA arrives for every stage, also where it has nothing to load: the leading
             // one must not get ahead of it, whose `empty` would pass a phase that it never saw.
+            // Relaxed: the copies' own completions order the data, and a release waits for all that
+            // this thread has in flight (1050 clocks a stage, twice what its MMAs take).
             if (rank == 0)
               mbar_arrive_expect_tx(smem_u32(&full[stage]), bytes);
             else
-              mbar_arrive_cluster(bar);
+              mbar_arrive_cluster_relaxed(bar);
             a.load(&map, sa, bar, kb);
             b.load(&map, sa + 2 * kOrthoBlk, bar, kb);
             ++issued;
