@@ -1678,8 +1678,8 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   p->ws = base;
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
-  size_t words = 4 + (size_t)count;
-  long long parts = 0, pack = 0, gram = 0, sym = 0, full = 0, blocks = 0;
+  const size_t words = 4 + (size_t)count;
+  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0, blocks = 0;
   for (int i = 0; i < count; ++i) {
     const OrthoEntry& s = e[order[i]];
     OrthoMat& m = p->mat[i];
@@ -1698,7 +1698,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     blocks += (long long)ortho_sym(ortho_tiles(m.mb)) * m.nb;
   }
   // X X^T's sums split so that an item's share is near a pair's share of them all, but no less
-  // than 12 blocks (about 3 us: a part costs its store and the last one all loads).
+  // than 12 blocks (about 3 us; the parts' store, their phase and its wait take about 8).
   const long long share = std::max(12ll, blocks / kOrthoPairs);
   for (int i = 0; i < count; ++i) {
     OrthoMat& m = p->mat[i];
@@ -1706,23 +1706,24 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     m.kper = cdiv(m.nb, m.splits);
     m.splits = cdiv(m.nb, m.kper);
     const int mt = ortho_tiles(m.mb), nt = ortho_tiles(m.nb), tri = ortho_sym(mt);
-    m.arrivals = p->ticket + words;
-    if (m.splits > 1) words += (size_t)tri * kOrthoSignals;
     p->pre_pack[i] = (int)pack;
     p->pre_gram[i] = (int)gram;
+    p->pre_sum[i] = (int)sum;
     p->pre_sym[i] = (int)sym;
     p->pre_full[i] = (int)full;
     pack += (long long)m.mb * m.nb;
     gram += (long long)tri * m.splits;
+    if (m.splits > 1) sum += (long long)tri * kOrthoSumItems;
     sym += tri;
     full += (long long)mt * nt;
   }
   p->pre_pack[count] = (int)pack;
   p->pre_gram[count] = (int)gram;
+  p->pre_sum[count] = (int)sum;
   p->pre_sym[count] = (int)sym;
   p->pre_full[count] = (int)full;
   p->total_parts = (int)parts;
-  p->max_items = (int)std::max(gram, full);
+  p->max_items = (int)std::max(std::max(gram, sum), full);
   p->zero_words = words;
   size_t at = round_up(words * 4, 256);
   p->parts = reinterpret_cast<float*>(base + at);

@@ -27,8 +27,8 @@
 // tcgen05.mma.cta_group::2: each CTA loads 128 rows of either operand, 64 bytes
 // a clock at the full MMA rate.  128 x 128 tiles of single CTAs need 128 and were
 // bound by the L2's 46 bytes a clock and SM (4096 x 4096: 2.34 ms).
-// X X^T of a wide matrix has few tiles and long sums: the sum is split over n,
-// and the part that arrives last adds all parts in order.
+// X X^T of a wide matrix has few tiles and long sums: the sum is split over n, and a
+// phase of its own, in items small enough for every SM to have one, adds the parts in order.
 //
 // Schedule.  After the norms and the packing, one persistent kernel runs all
 // phases of all matrices: work items (tiles of a product) are numbered phase by phase
@@ -59,10 +59,10 @@ constexpr int kThreads = 64 + kEpi;         // and a warp each for the loads and
 constexpr int kPackPitch = 65;
 constexpr int kOrthoSmem = 1024 + kStages * kStageBytes + 4 * kOrthoBlk;
 
-enum ItemKind : int { kGram = 1, kSym = 2, kFull = 3, kStop = 4 };
+enum ItemKind : int { kGram = 1, kSym = 2, kFull = 3, kSum = 4, kStop = 5 };
 struct __align__(16) Item {
   int kind, mat, I, J;
-  int step, k0, k1, split;  // blocks [k0, k1) of the sum, which part of it
+  int step, k0, k1, split;  // blocks [k0, k1) of the sum, which part of it (kSum: which columns)
 };
 
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
@@ -116,10 +116,10 @@ __device__ __forceinline__ void sym_tile(int local, int& I, int& J) {
 __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, uint32_t& need) {
   Item it;
   const int n = p.count;
-  const int tg = p.pre_gram[n], ts = p.pre_sym[n], tf = p.pre_full[n];
+  const int tg = p.pre_gram[n], ta = p.pre_sum[n], ts = p.pre_sym[n], tf = p.pre_full[n];
   it.k0 = it.split = 0;
   uint32_t t = ticket;
-  const uint32_t per = (uint32_t)(tg + ts + tf);
+  const uint32_t per = (uint32_t)(tg + ta + ts + tf);
   it.step = (int)(t / per);
   t -= (uint32_t)it.step * per;
   if (it.step >= p.steps) {
@@ -137,14 +137,22 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     sym_tile(local / M.splits, it.I, it.J);
     it.k0 = it.split * M.kper;
     it.k1 = min(it.k0 + M.kper, M.nb);
-  } else if (t < (uint32_t)(tg + ts)) {
+  } else if (t < (uint32_t)(tg + ta)) {
     t -= (uint32_t)tg;
+    it.kind = kSum;
+    it.mat = find_mat(p.pre_sum, n, (int)t);
+    const int local = (int)t - p.pre_sum[it.mat];
+    it.split = local % kOrthoSumItems;
+    sym_tile(local / kOrthoSumItems, it.I, it.J);
+    it.k1 = 0;
+  } else if (t < (uint32_t)(tg + ta + ts)) {
+    t -= (uint32_t)(tg + ta);
     it.kind = kSym;
     it.mat = find_mat(p.pre_sym, n, (int)t);
     sym_tile((int)t - p.pre_sym[it.mat], it.I, it.J);
     it.k1 = p.mat[it.mat].mb;
   } else {
-    t -= (uint32_t)(tg + ts);
+    t -= (uint32_t)(tg + ta + ts);
     it.kind = kFull;
     it.mat = find_mat(p.pre_full, n, (int)t);
     const int local = (int)t - p.pre_full[it.mat];
@@ -155,8 +163,13 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
   }
   const OrthoMat& M = p.mat[it.mat];
   const int mt = ortho_tiles(M.mb), nt = ortho_tiles(M.nb);
-  const uint32_t sym = (uint32_t)ortho_sym(mt);
-  need = kOrthoSignals * ((uint32_t)it.step * (2 * sym + (uint32_t)(mt * nt)) + (uint32_t)(it.kind - kGram) * sym);
+  const uint32_t tri = (uint32_t)ortho_sym(mt), gram = tri * (uint32_t)M.splits;
+  const uint32_t sum = M.splits > 1 ? tri * kOrthoSumItems : 0;
+  uint32_t before = (uint32_t)it.step * (gram + sum + tri + (uint32_t)(mt * nt));
+  if (it.kind != kGram) before += gram;
+  if (it.kind == kSym || it.kind == kFull) before += sum;
+  if (it.kind == kFull) before += tri;
+  need = kOrthoSignals * before;
   return it;
 }
 
@@ -701,6 +714,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           rphase ^= 1;
         }
         if (it.kind == kStop) break;
+        if (it.kind == kSum) continue;
         fence_proxy_async_all();  // the blocks' writers used both proxies
         const OrthoMat& M = p.mat[it.mat];
         const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
@@ -772,6 +786,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           rphase ^= 1;
         }
         if (it.kind == kStop) break;
+        if (it.kind == kSum) continue;
         const bool same = it.kind != kFull && it.I == it.J;
         if (!mbar_wait_cluster(smem_u32(&acc_empty[acc]), aphase ^ 1, 2 * lim)) {
           record_timeout(p.status, abort_flag);
@@ -858,6 +873,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         : it.kind == kSym ? kC * kSb / (kSa * kSa)
                                           : 1.f / (kSx * kSb);
       const TileOut o{p, M, it, out, a16, x32, mul, stage_w, chunks, rr, lane, row, bj0, full_kind, final_step};
+      // FP32 parts of a split sum: this warp's rows and columns, four columns a lane at a time
+      float4* part = reinterpret_cast<float4*>(
+                         M.ws + L.part +
+                         ((size_t)(ortho_sym(it.I) + it.J) * M.splits * kOrthoSignals + rank * 8 + ew) * kOrthoPart) +
+                     lane;
+      constexpr int kNext = kOrthoSignals * kOrthoPart / 16;  // to the next part
+      if (it.kind == kSum) {
+        if (it.split * 16 < chunks * 32) {
+          float x[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[j] = 0.f;
+#pragma unroll 8
+          for (int s = 0; s < M.splits; ++s) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float4 f = __ldcg(part + s * kNext + (it.split * 4 + j) * 32);
+              x[4 * j] += f.x;
+              x[4 * j + 1] += f.y;
+              x[4 * j + 2] += f.z;
+              x[4 * j + 3] += f.w;
+            }
+          }
+          const float mul_a = kSa / (kSx * kSx);
+          uint32_t h[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) h[j] = f2h2(x[2 * j] * mul_a, x[2 * j + 1] * mul_a);
+          uint8_t* dst = const_cast<uint8_t*>(a16) + (it.split >> 2) * (2 * kOrthoBlk);
+          const int ch = (it.split & 3) * 2;
+          __stcg(reinterpret_cast<uint4*>(dst + ((ch ^ (rr & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
+          __stcg(reinterpret_cast<uint4*>(dst + (((ch + 1) ^ (rr & 7)) << 4)), make_uint4(h[4], h[5], h[6], h[7]));
+          fence_proxy_async_all();  // the operand copies read them
+        }
+        __syncwarp();
+        if (lane == 0) red_release_add(p.done + it.mat, 1u);
+        continue;
+      }
       // two chunks' addends are loaded while the product runs (the item's dependency, which the
       // loading warp has seen, covers them), the others' as registers come free
       uint4 va[8], vb[8];
@@ -869,56 +920,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       tc_fence_after();
       const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * 128);
-      bool signal = any || it.split == 0;
       if (it.kind == kGram && M.splits > 1) {
-        if (any) {
-          // this part of the sum; the last part to arrive adds them all, in order
-          const int slice = (ortho_sym(it.I) + it.J) * kOrthoSignals + (int)rank * 8 + ew;
-          float4* part = reinterpret_cast<float4*>(
-                             M.ws + L.part +
-                             ((size_t)(ortho_sym(it.I) + it.J) * M.splits * kOrthoSignals + rank * 8 + ew) *
-                                 kOrthoPart) + lane;
-          constexpr int kNext = kOrthoSignals * kOrthoPart / 16;  // float4s to the next part
 #pragma unroll 1
-          for (int c = 0; c < chunks; ++c) {
-            uint32_t r[32];
-            product(tacc, c, r);
+        for (int c = 0; c < chunks; ++c) {
+          uint32_t r[32];
+          product(tacc, c, r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              __stcg(part + it.split * kNext + (c * 8 + j) * 32,
-                     make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]),
-                                 __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3])));
-          }
-          uint32_t seen = 0;
-          __syncwarp();
-          if (lane == 0) {
-            __threadfence();
-            seen = atomicAdd(M.arrivals + slice, 1u);
-            __threadfence();
-          }
-          seen = __shfl_sync(0xffffffffu, seen, 0);
-          __syncwarp();
-          signal = seen % (uint32_t)M.splits == (uint32_t)M.splits - 1;
-          if (signal) {
-#pragma unroll 1
-            for (int c = 0; c < chunks; ++c) {
-              uint32_t x[32];
-#pragma unroll
-              for (int j = 0; j < 32; ++j) x[j] = 0;
-#pragma unroll 3
-              for (int s = 0; s < M.splits; ++s) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const float4 f = __ldcg(part + s * kNext + (c * 8 + j) * 32);
-                  x[4 * j] = __float_as_uint(__uint_as_float(x[4 * j]) + f.x);
-                  x[4 * j + 1] = __float_as_uint(__uint_as_float(x[4 * j + 1]) + f.y);
-                  x[4 * j + 2] = __float_as_uint(__uint_as_float(x[4 * j + 2]) + f.z);
-                  x[4 * j + 3] = __float_as_uint(__uint_as_float(x[4 * j + 3]) + f.w);
-                }
-              }
-              o.store(c, x, va);
-            }
-          }
+          for (int j = 0; j < 8; ++j)
+            __stcg(part + it.split * kNext + (c * 8 + j) * 32,
+                   make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]),
+                               __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3])));
         }
       } else {
         uint32_t r[32];
@@ -941,10 +952,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) {
         mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
-        if (signal) {
-          bulk_wait0();
-          red_release_add(p.done + it.mat, 1u);
-        }
+        bulk_wait0();
+        red_release_add(p.done + it.mat, 1u);
       }
       __syncwarp();
       acc ^= 1;

@@ -20,7 +20,6 @@ struct OrthoMat {
   uint16_t* v;        // momentum (null: plain orthogonalisation)
   uint16_t* w;        // weights updated in place, or the output
   uint8_t* ws;        // x16[2], x32, a16, b16, split sums (ortho_layout)
-  uint32_t* arrivals; // of the split sums
   int rows, cols;     // as the caller sees it
   int mb, nb;
   int part0, parts;   // its partial sums of squares
@@ -43,9 +42,9 @@ struct OrthoParams {
   int* status;
   unsigned long long wait_limit_ns;
   int pre_pack[kOrthoMax + 1];  // first block of each matrix, and their number
-  // first item of each matrix within each kind of phase (X X^T, the
+  // first item of each matrix within each kind of phase (X X^T, the sums of its parts, the
   // symmetric product of S, the full product); entry `count` is the kind's total
-  int pre_gram[kOrthoMax + 1], pre_sym[kOrthoMax + 1], pre_full[kOrthoMax + 1];
+  int pre_gram[kOrthoMax + 1], pre_sum[kOrthoMax + 1], pre_sym[kOrthoMax + 1], pre_full[kOrthoMax + 1];
   OrthoMat mat[kOrthoMax];
 };
 
@@ -56,9 +55,10 @@ constexpr int kOrthoPairs = 76;      // of SMs
 __host__ __device__ inline int ortho_tiles(int blocks) { return (blocks + 3) >> 2; }
 __host__ __device__ inline int ortho_sym(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Split sums of X X^T: FP32 parts [tile][split][CTA of the pair][warp], 16 KB each, and an
-// arrival counter for each [tile][CTA of the pair][warp].
+// Split sums of X X^T: FP32 parts [tile][split][CTA of the pair][warp], 16 KB each, added in items of
+// 16 of each warp's 128 columns.
 constexpr int kOrthoPart = 16384;
+constexpr int kOrthoSumItems = 8;
 
 struct OrthoLayout {
   size_t x16, x32, a16, b16, part, bytes;
