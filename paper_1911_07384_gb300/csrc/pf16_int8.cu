@@ -51,94 +51,124 @@ __device__ __forceinline__ float stored_scale(float a) {
 
 }  // namespace
 
-// One row by each group of G threads (G <= 32: part of a warp; 256: the CTA).
+// R rows by each group of G threads (G <= 32: part of a warp; 256: the CTA).
 // VEC: rows of whole 16-byte vectors, of which a thread keeps its first KEEP in registers between the
 // maximum and the rounding and reads the others twice.
-template <int G, int KEEP, bool VEC>
+// Bound by memory: every load of a thread's rows is issued before the first maximum is taken.
+template <int G, int KEEP, int R, bool VEC>
 __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict__ x, int8_t* __restrict__ q,
                                                      float* __restrict__ scale, long long m, int k) {
   pdl_wait();
-  constexpr int ROWS = 256 / G;
+  constexpr int GROUPS = 256 / G;
   const int g = (int)threadIdx.x % G;
-  const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / G;
-  const bool live = row < m;
-  const uint16_t* xr = x + (live ? row : 0) * k;
-  uint4 keep[KEEP > 0 ? KEEP : 1];
-  uint32_t mx = 0;
+  const long long row0 = (long long)blockIdx.x * (GROUPS * R) + threadIdx.x / G;  // and every GROUPS-th from there
+  const int nv = k >> 3;
+  uint4 keep[R][KEEP > 0 ? KEEP : 1];
+  uint32_t mx[R];
   if (VEC) {
-    const int nv = live ? k >> 3 : 0;
-    const uint4* xv = reinterpret_cast<const uint4*>(xr);
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      keep[i] = g + i * G < nv ? __ldcs(xv + g + i * G) : make_uint4(0, 0, 0, 0);
+    for (int r = 0; r < R; ++r) {
+      const long long row = row0 + r * GROUPS;
+      const uint4* xv = reinterpret_cast<const uint4*>(x + (row < m ? row : 0) * k);
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, keep[i].x), keep[i].y), keep[i].z), keep[i].w);
-    for (int c = g + KEEP * G; c < nv; c += G) {
-      const uint4 v = xv[c];
-      mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, v.x), v.y), v.z), v.w);
+      for (int i = 0; i < KEEP; ++i)
+        keep[r][i] = row < m && g + i * G < nv ? __ldcs(xv + g + i * G) : make_uint4(0, 0, 0, 0);
     }
-  } else {
-    for (int c = g; c < (live ? k : 0); c += G) mx = abs_max2(mx, (uint32_t)xr[c]);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const long long row = row0 + r * GROUPS;
+    const uint16_t* xr = x + (row < m ? row : 0) * k;
+    uint32_t v = 0;
+    if (VEC) {
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i)
+        v = abs_max2(abs_max2(abs_max2(abs_max2(v, keep[r][i].x), keep[r][i].y), keep[r][i].z), keep[r][i].w);
+      for (int c = g + KEEP * G; c < (row < m ? nv : 0); c += G) {
+        const uint4 u = reinterpret_cast<const uint4*>(xr)[c];
+        v = abs_max2(abs_max2(abs_max2(abs_max2(v, u.x), u.y), u.z), u.w);
+      }
+    } else {
+      for (int c = g; c < (row < m ? k : 0); c += G) v = abs_max2(v, (uint32_t)xr[c]);
+    }
+    mx[r] = v;
   }
   constexpr int W = G < 32 ? G : 32;
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) mx = abs_max2(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-  mx = abs_max2(mx, mx >> 16);
+  for (int o = W / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int r = 0; r < R; ++r) mx[r] = abs_max2(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], o));
+#pragma unroll
+  for (int r = 0; r < R; ++r) mx[r] = abs_max2(mx[r], mx[r] >> 16);
   if (G > 32) {
-    __shared__ uint32_t red[8];
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mx;
+    __shared__ uint32_t red[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if ((threadIdx.x & 31) == 0) red[r][threadIdx.x >> 5] = mx[r];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mx = abs_max2(mx, red[i]);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx[r] = abs_max2(mx[r], red[r][i]);
   }
-  if (!live) return;
-  const float a = h2f((uint16_t)mx);
-  const RowScale s = row_scale(a);
-  if (g == 0) scale[row] = stored_scale(a);
-  int8_t* qr = q + row * k;
-  // with r = 0 (a zero row, or one that is not finite) the integers are zero
-  if (VEC) {
-    const int nv = k >> 3;
-    const uint4* xv = reinterpret_cast<const uint4*>(xr);
-    auto put = [&](int c, const uint4& v) {
-      const uint32_t* h = reinterpret_cast<const uint32_t*>(&v);
-      uint2 o = make_uint2(0, 0);
-      if (s.r != 0.f) {
-        uint32_t b[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          b[2 * j] = quant1((uint16_t)h[j], s);
-          b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
+  for (int r = 0; r < R; ++r) {
+    const long long row = row0 + r * GROUPS;
+    if (row >= m) break;
+    const uint16_t* xr = x + row * k;
+    const float a = h2f((uint16_t)mx[r]);
+    const RowScale s = row_scale(a);
+    if (g == 0) scale[row] = stored_scale(a);
+    int8_t* qr = q + row * k;
+    // with r = 0 (a zero row, or one that is not finite) the integers are zero
+    if (VEC) {
+      const uint4* xv = reinterpret_cast<const uint4*>(xr);
+      auto put = [&](int c, const uint4& v) {
+        const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+        uint2 o = make_uint2(0, 0);
+        if (s.r != 0.f) {
+          uint32_t b[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            b[2 * j] = quant1((uint16_t)h[j], s);
+            b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
+          }
+          o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
+          o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
         }
-        o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
-        o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
-      }
-      __stcs(reinterpret_cast<uint2*>(qr) + c, o);
-    };
+        __stcs(reinterpret_cast<uint2*>(qr) + c, o);
+      };
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      if (g + i * G < nv) put(g + i * G, keep[i]);
-    for (int c = g + KEEP * G; c < nv; c += G) put(c, xv[c]);
-  } else {
-    for (int c = g; c < k; c += G) qr[c] = s.r != 0.f ? (int8_t)quant1(xr[c], s) : (int8_t)0;
+      for (int i = 0; i < KEEP; ++i)
+        if (g + i * G < nv) put(g + i * G, keep[r][i]);
+      for (int c = g + KEEP * G; c < nv; c += G) put(c, xv[c]);
+    } else {
+      for (int c = g; c < k; c += G) qr[c] = s.r != 0.f ? (int8_t)quant1(xr[c], s) : (int8_t)0;
+    }
   }
 }
 
-template <int G, int KEEP>
+template <int G, int KEEP, int R>
 static cudaError_t quantize_g(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s) {
-  const long long blocks = (m + 256 / G - 1) / (256 / G);
-  const dim3 grid((unsigned)blocks), block(256);
-  const cudaError_t e = (k & 7) == 0 ? launch_pdl(k_quantize_i8<G, KEEP, true>, grid, block, 0, s, x, q, scale, m, k)
-                                     : launch_pdl(k_quantize_i8<G, 0, false>, grid, block, 0, s, x, q, scale, m, k);
+  const long long rows = 256 / G * R;
+  const dim3 grid((unsigned)((m + rows - 1) / rows)), block(256);
+  const cudaError_t e = (k & 7) == 0
+                            ? launch_pdl(k_quantize_i8<G, KEEP, R, true>, grid, block, 0, s, x, q, scale, m, k)
+                            : launch_pdl(k_quantize_i8<G, 0, R, false>, grid, block, 0, s, x, q, scale, m, k);
   return e == cudaSuccess ? counted_launches(1) : e;
 }
 
 cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s) {
-  if (k <= 64) return quantize_g<8, 1>(x, q, scale, m, k, s);
-  if (k <= 128) return quantize_g<16, 1>(x, q, scale, m, k, s);
-  if (k <= 1024) return quantize_g<32, 4>(x, q, scale, m, k, s);
-  return quantize_g<256, 4>(x, q, scale, m, k, s);
+  // Few lanes a row and four vectors a lane: what a row costs apart from its elements (its reduction and two
+  // divisions, by all its lanes) took longer than memory with a warp a row (802816 x 256: 130 us).
+  if (k <= 64) return quantize_g<2, 4, 1>(x, q, scale, m, k, s);
+  if (k <= 128) return quantize_g<4, 4, 1>(x, q, scale, m, k, s);
+  if (k <= 256) return quantize_g<8, 4, 1>(x, q, scale, m, k, s);
+  if (k <= 512) return quantize_g<16, 4, 1>(x, q, scale, m, k, s);
+  if (k <= 1024) return quantize_g<32, 4, 1>(x, q, scale, m, k, s);
+  if (k <= 2048) return m < 2048 ? quantize_g<256, 1, 1>(x, q, scale, m, k, s) : quantize_g<256, 1, 4>(x, q, scale, m, k, s);
+  if (k <= 4096) return quantize_g<256, 2, 1>(x, q, scale, m, k, s);
+  return quantize_g<256, 8, 1>(x, q, scale, m, k, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -473,6 +503,235 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
   }
 }
 
+// ---------------------------------------------------------------------------
+// The same for many rows of x: persistent CTAs, x as P and w as Q, the
+// accumulators of two tiles in tensor memory, so that four warps scale and store
+// one tile while the others convert and multiply the next.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kBigThreads = 32 * 13;  // MMA, four storing warps, eight converting warps
+
+template <int BN>
+struct BigCfg {
+  static constexpr int STAGE = (128 + BN) * 128;
+  static constexpr int STAGES = BN >= 256 ? 4 : BN >= 128 ? 6 : 8;
+  static constexpr int DIST = BN >= 256 ? 3 : BN >= 128 ? 4 : 6;  // K-blocks of raw bytes in registers
+  static constexpr int UQ = BN / 64;
+  static constexpr int U = 2 + UQ;
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * 4096 + 2 * BN * 8;
+};
+
+}  // namespace
+
+template <int BN, bool ALIGNED>
+__global__ void __launch_bounds__(kBigThreads, 1)
+    k_linear_i8_big(const LinearI8 a, int q_tiles, int tiles, int* status, unsigned long long lim) {
+  using Cfg = BigCfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* staging = smem + Cfg::STAGES * Cfg::STAGE;                 // 4 KB a storing warp
+  float2* swb = reinterpret_cast<float2*>(staging + 4 * 4096);        // [2][BN] scale and bias of a channel
+  __shared__ uint64_t full[Cfg::STAGES], empty[Cfg::STAGES], acc_full[2], acc_empty[2], last;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int drained;
+  const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < Cfg::STAGES; ++i) {
+      mbar_init(smem_u32(&full[i]), 8);
+      mbar_init(smem_u32(&empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&acc_full[i]), 1);
+      mbar_init(smem_u32(&acc_empty[i]), 4);
+    }
+    mbar_init(smem_u32(&last), 1);
+    drained = 1;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(&tmem_slot), 2 * BN);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = tmem_slot;
+  const int nk = (a.k + 63) >> 6;
+  const int mine = ((int)blockIdx.x < tiles ? (tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0);
+
+  if (warp == 0) {
+    if (elect_one()) {
+      const uint64_t desc = smem_desc(0, 16, 1024, 2);
+      const uint32_t idesc = idesc_f16(128, BN, false, false, true);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int n = 0; n < mine && ok; ++n) {
+        const int acc = n & 1;
+        ok = mbar_wait(smem_u32(&acc_empty[acc]), ((n >> 1) & 1) ^ 1, lim);
+        if (!ok) break;
+        tc_fence_after();
+        for (int i = 0; i < nk; ++i) {
+          ok = mbar_wait(smem_u32(&full[stage]), phase, lim);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE));
+          const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            tc_mma_f16(tmem + (uint32_t)(acc * BN), ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc,
+                       i > 0 || kk > 0);
+          tc_commit(smem_u32(&empty[stage]));
+          if (++stage == Cfg::STAGES) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        if (ok) tc_commit(smem_u32(&acc_full[acc]));
+      }
+      if (!ok) atomicCAS(status, 0, -7);  // PF16_ERR_TIMEOUT
+      tc_commit(smem_u32(&last));  // nothing runs in TMEM when it is released
+      if (!mbar_wait(smem_u32(&last), 0, lim)) drained = 0;
+    }
+    __syncwarp();
+  } else if (warp <= 4) {
+    const int quad = warp & 3, et = tid - 32;
+    const uint32_t stage_w = smem_u32(staging + (warp - 1) * 4096);
+    const bool vec = (a.n & 7) == 0;
+    for (int n = 0; n < mine; ++n) {
+      const int acc = n & 1, tile = (int)blockIdx.x + n * (int)gridDim.x;
+      const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
+      // this tile's channel scales and biases; the other buffer may still be read
+      for (int j = et; j < BN; j += 128) {
+        const int q = q0 + j;
+        swb[acc * BN + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const int row = p0 + quad * 32 + lane;
+      const float sx = row < a.m ? a.sx[row] : 0.f;
+      if (!mbar_wait(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
+        atomicCAS(status, 0, -7);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
+#pragma unroll 1
+      for (int c = 0; c < BN; c += 64) {
+        if (q0 + c >= a.n) break;
+#pragma unroll
+        for (int h = 0; h < 64; h += 32) {
+          uint32_t r[32];
+          tmem_ld16(tacc + (uint32_t)(c + h), r);
+          tmem_ld16(tacc + (uint32_t)(c + h + 16), r + 16);
+          tmem_ld_wait();
+          const float4* sb = reinterpret_cast<const float4*>(swb + acc * BN + c + h);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float4 f = sb[j * 4 + q];  // two channels
+              o[q] = f2h2(fmaf(__uint_as_float(r[8 * j + 2 * q]), sx * f.x, f.y),
+                          fmaf(__uint_as_float(r[8 * j + 2 * q + 1]), sx * f.z, f.w));
+            }
+            st_shared_v4(stage_w + (uint32_t)(lane * 128 + (((h / 8 + j) ^ (lane & 7)) << 4)),
+                         make_uint4(o[0], o[1], o[2], o[3]));
+          }
+        }
+        __syncwarp();
+        // 32 rows of 64 channels, whole 128-byte rows at a time
+        const int left = a.n - q0 - c, r0 = p0 + quad * 32;
+        if (vec) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int rr = i * 4 + (lane >> 3), ch = lane & 7;
+            uint4 v;
+            ld_shared_v4(stage_w + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)), v);
+            if (r0 + rr < a.m && ch * 8 < left)
+              *reinterpret_cast<uint4*>(a.y + (long long)(r0 + rr) * a.n + q0 + c + ch * 8) = v;
+          }
+        } else {
+          const uint16_t* sp = reinterpret_cast<const uint16_t*>(staging + (warp - 1) * 4096);
+          for (int i = 0; i < 64; ++i) {
+            const int rr = i >> 1, e = (i & 1) * 32 + lane;
+            if (r0 + rr < a.m && e < left)
+              a.y[(long long)(r0 + rr) * a.n + q0 + c + e] = sp[rr * 64 + (((e >> 3) ^ (rr & 7)) << 3) + (e & 7)];
+          }
+        }
+        __syncwarp();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
+    }
+  } else {
+    const int ct = tid - 160, c = ct & 3;
+    const int8_t* base[Cfg::U];
+    bool live[Cfg::U];
+    auto place = [&](int n) {  // this thread's rows in the n-th tile
+      const int tile = (int)blockIdx.x + n * (int)gridDim.x;
+      const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
+#pragma unroll
+      for (int i = 0; i < Cfg::U; ++i) {
+        const int row = (i < 2 ? p0 + i * 64 : q0 + (i - 2) * 64) + (ct >> 2);
+        live[i] = n < mine && row < (i < 2 ? a.m : a.n);
+        base[i] = (i < 2 ? a.x : a.w) + (long long)(live[i] ? row : 0) * a.k;
+      }
+    };
+    uint4 raw[Cfg::DIST][Cfg::U];
+    int fn = 0, fk = 0;  // the next K-block to fetch
+    place(0);
+    auto fetch = [&](uint4* dst) {
+      const int at = fk * 64 + c * 16;
+#pragma unroll
+      for (int u = 0; u < Cfg::U; ++u)
+        dst[u] = live[u] ? load16<ALIGNED>(base[u], at, a.k) : make_uint4(0, 0, 0, 0);
+      if (++fk == nk) {
+        fk = 0;
+        place(++fn);
+      }
+    };
+#pragma unroll
+    for (int d = 0; d < Cfg::DIST; ++d) fetch(raw[d]);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const long long total = (long long)mine * nk;
+    for (long long i = 0; ok && i < total; i += Cfg::DIST) {
+#pragma unroll
+      for (int d = 0; d < Cfg::DIST; ++d) {
+        if (i + d >= total) break;
+        ok = mbar_wait(smem_u32(&empty[stage]), phase ^ 1, lim);
+        if (!ok) {
+          atomicCAS(status, 0, -7);
+          break;
+        }
+        const uint32_t sp = smem_u32(smem + stage * Cfg::STAGE), sq = sp + 128 * 128;
+#pragma unroll
+        for (int u = 0; u < Cfg::U; ++u)
+          put16(u < 2 ? sp : sq, (ct >> 2) + (u < 2 ? u : u - 2) * 64, c, raw[d][u]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
+        fetch(raw[d]);
+        if (++stage == Cfg::STAGES) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0 && drained) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 2 * BN);
+  }
+}
+
 namespace {
 
 template <int BN, bool SWAP, bool ALIGNED>
@@ -506,6 +765,26 @@ cudaError_t linear_al(const LinearI8& a, int splits, int* status, cudaStream_t s
                          : linear_mma<BN, SWAP, false>(a, splits, status, s);
 }
 
+template <int BN, bool ALIGNED>
+cudaError_t linear_big_al(const LinearI8& a, int sms, int* status, cudaStream_t s) {
+  using Cfg = BigCfg<BN>;
+  auto kernel = k_linear_i8_big<BN, ALIGNED>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM);
+  if (e != cudaSuccess) return e;
+  const int q_tiles = (a.n + BN - 1) / BN;
+  const long long tiles = (long long)((a.m + 127) / 128) * q_tiles;
+  if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
+  const int grid = tiles < sms ? (int)tiles : sms;
+  e = launch_pdl(kernel, dim3((unsigned)grid), dim3(kBigThreads), Cfg::SMEM, s, a, q_tiles, (int)tiles, status,
+                 4000000000ull);
+  return e == cudaSuccess ? counted_launches(1) : e;
+}
+
+template <int BN>
+cudaError_t linear_big(const LinearI8& a, int sms, int* status, cudaStream_t s) {
+  return (a.k & 15) == 0 ? linear_big_al<BN, true>(a, sms, status, s) : linear_big_al<BN, false>(a, sms, status, s);
+}
+
 template <int MT>
 cudaError_t linear_rows(const LinearI8& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)((a.m + MT - 1) / MT));
@@ -535,9 +814,12 @@ cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream
   switch (bn) {
     case 16: return linear_al<16, true>(a, splits, status, s);
     case 32: return linear_al<32, true>(a, splits, status, s);
-    case 64: return swap ? linear_al<64, true>(a, splits, status, s) : linear_al<64, false>(a, splits, status, s);
-    case 128: return linear_al<128, false>(a, splits, status, s);
-    default: return linear_al<256, false>(a, splits, status, s);
+    case 64:
+      if (swap) return linear_al<64, true>(a, splits, status, s);
+      if (splits > 1) return linear_al<64, false>(a, splits, status, s);
+      return linear_big<64>(a, sms, status, s);
+    case 128: return linear_big<128>(a, sms, status, s);
+    default: return linear_big<256>(a, sms, status, s);
   }
 }
 
