@@ -19,7 +19,8 @@ LIB = os.path.join(BUILD, "libpf16.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 SOURCES = ["pf16_api.cu", "pf16_gemm.cu", "pf16_halo.cu", "pf16_elementwise.cu", "pf16_noalloc.cu", "pf16_probe.cu",
            "pf16_ortho.cu", "pf16_int8.cu"]
-HEADERS = ["pf16_internal.h", "pf16_plan.h", "pf16_ptx.cuh", "pf16_epi.cuh", "pf16_ortho.h", "pf16_int8.h"]
+HEADERS = ["pf16_internal.h", "pf16_plan.h", "pf16_ptx.cuh", "pf16_epi.cuh", "pf16_pair.cuh", "pf16_ortho.h",
+           "pf16_int8.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
          "--expt-relaxed-constexpr", "-I", INCLUDE]

@@ -1856,7 +1856,7 @@ int pf16_quantize_i8(const uint16_t* x, int8_t* q, float* scale, int32_t m, int3
 
 int pf16_linear_i8(const int8_t* x, const float* sx, const int8_t* w, const float* sw, const uint16_t* bias,
                    uint16_t* y, int32_t m, int32_t n, int32_t k, void* stream) {
-  if (m < 0 || n < 1 || k < 1 || k > 65536) return PF16_ERR_SHAPE;
+  if (m < 0 || n < 1 || k < 1 || m > (1 << 30) || n > (1 << 30) || k > 65536) return PF16_ERR_SHAPE;
   if (m == 0) return PF16_OK;
   if (!x || !sx || !w || !sw || !y) return PF16_ERR_NULL;
   if (!aligned16(x) || !aligned16(w) || !aligned16(y) || (reinterpret_cast<uintptr_t>(sx) & 3u) ||

@@ -5,6 +5,7 @@
 
 #include "pf16_int8.h"
 #include "pf16_internal.h"
+#include "pf16_pair.cuh"
 #include "pf16_ptx.cuh"
 
 namespace pf16 {
@@ -282,14 +283,6 @@ __device__ __forceinline__ void put16(uint32_t tile, int row, int c, const uint4
   st_shared_v4(at + (uint32_t)(((2 * c) ^ (row & 7)) << 4), make_uint4(a.x, a.y, b.x, b.y));
   st_shared_v4(at + (uint32_t)(((2 * c + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
 }
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ float ld_cluster(uint32_t saddr, uint32_t rank) {
   uint32_t a;
   float v;
@@ -512,15 +505,124 @@ namespace {
 
 constexpr int kBigThreads = 32 * 13;  // MMA, four storing warps, eight converting warps
 
+// A stage is 128 values of K, two K-blocks of swizzled tiles: eight lanes load 128 bytes of a row, whole
+// lines.  With four lanes a row (64 bytes) the loads' tags and the stores' data took 770 of the L1's cycles
+// for each 512 of the MMAs.
 template <int BN>
 struct BigCfg {
-  static constexpr int STAGE = (128 + BN) * 128;
-  static constexpr int STAGES = BN >= 256 ? 4 : BN >= 128 ? 6 : 8;
-  static constexpr int DIST = BN >= 256 ? 3 : BN >= 128 ? 4 : 6;  // K-blocks of raw bytes in registers
-  static constexpr int UQ = BN / 64;
-  static constexpr int U = 2 + UQ;
+  static constexpr int HALF = (128 + BN) * 128;  // one K-block: P's tile, then Q's
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int STAGES = BN >= 256 ? 2 : BN >= 128 ? 3 : 4;
+  static constexpr int DIST = BN >= 128 ? 2 : 3;  // stages of raw bytes in registers
+  static constexpr int UP = 4, U = UP + BN / 32;  // 16-byte units of P, of both, that a thread loads per stage
   static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * 4096 + 2 * BN * 8;
 };
+
+// A converting thread's share of the operands: unit u of a stage is bytes 16 (ct & 7) of row (ct >> 3) + 32 u of
+// P, or of row (ct >> 3) + 32 (u - UP) of Q.  The raw bytes of DIST stages are in registers.
+// Tile t of this CTA has its rows of P from p0 + ..., given by the caller (`first`, as rows of x and w).
+template <int UP, int U, bool ALIGNED>
+struct Feed {
+  const LinearI8& a;
+  const int ct, tiles, ns, step_tile, q_tiles, pm, qm, pofs, qofs;
+  int tile, n, s;  // of the next stage to fetch: the tile, how many tiles before it, the stage in it
+  const int8_t *pb, *qb;
+  int pl, ql;      // rows from this thread's first to the end
+  const long long step;
+
+  // tiles first, first + step_tile, ...; tile t covers rows pm (t / q_tiles) + pofs of x and qm (t % q_tiles) + qofs
+  // of w
+  __device__ __forceinline__ Feed(const LinearI8& a_, int ct_, int first, int step_tile_, int tiles_, int ns_,
+                                  int q_tiles_, int pm_, int qm_, int pofs_, int qofs_)
+      : a(a_), ct(ct_), tiles(tiles_), ns(ns_), step_tile(step_tile_), q_tiles(q_tiles_), pm(pm_), qm(qm_),
+        pofs(pofs_), qofs(qofs_), tile(first), n(0), s(0), step(32ll * a_.k) {
+    place();
+  }
+  __device__ __forceinline__ void place() {
+    const int pr = (tile / q_tiles) * pm + pofs + (ct >> 3), qr = (tile % q_tiles) * qm + qofs + (ct >> 3);
+    pl = n < tiles ? a.m - pr : 0;
+    ql = n < tiles ? a.n - qr : 0;
+    pb = a.x + (pl > 0 ? (long long)pr * a.k : 0);
+    qb = a.w + (ql > 0 ? (long long)qr * a.k : 0);
+  }
+  __device__ __forceinline__ void fetch(int u, uint4& dst) const {  // (u is a constant where this is expanded)
+    const bool p = u < UP;
+    const int i = p ? u : u - UP;
+    dst = i * 32 < (p ? pl : ql) ? load16<ALIGNED>((p ? pb : qb) + i * step, s * 128 + (ct & 7) * 16, a.k)
+                                 : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void next() {
+    if (++s == ns) {
+      s = 0;
+      ++n;
+      tile += step_tile;
+      place();
+    }
+  }
+  // converts a stage into its two K-blocks' tiles at `half` (P's, then Q's) and fetches a later one in its place
+  __device__ __forceinline__ void convert(uint4 (&raw)[U], uint32_t half) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      put16(half + (u < UP ? 0 : 128 * 128), (ct >> 3) + (u < UP ? u : u - UP) * 32, ct & 3, raw[u]);
+      fetch(u, raw[u]);
+    }
+    next();
+    fence_proxy_async_smem();
+    __syncwarp();
+  }
+};
+
+// One storing warp's 32 rows (from r0 on) of a tile of BN channels (from q0 on): scaled, rounded, and
+// through 4 KB of shared memory into whole rows of 64 channels.
+template <int BN>
+__device__ __forceinline__ void store_tile(const LinearI8& a, uint32_t tacc, const float2* swb, uint32_t stage_w,
+                                           const uint8_t* stage_p, int r0, int q0, float sx, int lane) {
+#pragma unroll 1
+  for (int c = 0; c < BN; c += 64) {
+    if (q0 + c >= a.n) break;
+#pragma unroll
+    for (int h = 0; h < 64; h += 32) {
+      uint32_t r[32];
+      tmem_ld16(tacc + (uint32_t)(c + h), r);
+      tmem_ld16(tacc + (uint32_t)(c + h + 16), r + 16);
+      tmem_ld_wait();
+      const float4* sb = reinterpret_cast<const float4*>(swb + c + h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 f = sb[j * 4 + q];  // two channels
+          o[q] = f2h2(fmaf(__uint_as_float(r[8 * j + 2 * q]), sx * f.x, f.y),
+                      fmaf(__uint_as_float(r[8 * j + 2 * q + 1]), sx * f.z, f.w));
+        }
+        st_shared_v4(stage_w + (uint32_t)(lane * 128 + (((h / 8 + j) ^ (lane & 7)) << 4)),
+                     make_uint4(o[0], o[1], o[2], o[3]));
+      }
+    }
+    __syncwarp();
+    // 32 rows of 64 channels, whole 128-byte rows at a time
+    const int left = a.n - q0 - c;
+    if ((a.n & 7) == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int rr = i * 4 + (lane >> 3), ch = lane & 7;
+        uint4 v;
+        ld_shared_v4(stage_w + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)), v);
+        if (r0 + rr < a.m && ch * 8 < left)
+          *reinterpret_cast<uint4*>(a.y + (long long)(r0 + rr) * a.n + q0 + c + ch * 8) = v;
+      }
+    } else {
+      const uint16_t* sp = reinterpret_cast<const uint16_t*>(stage_p);
+      for (int i = 0; i < 64; ++i) {
+        const int rr = i >> 1, e = (i & 1) * 32 + lane;
+        if (r0 + rr < a.m && e < left)
+          a.y[(long long)(r0 + rr) * a.n + q0 + c + e] = sp[rr * 64 + (((e >> 3) ^ (rr & 7)) << 3) + (e & 7)];
+      }
+    }
+    __syncwarp();
+  }
+}
 
 }  // namespace
 
@@ -559,7 +661,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   tc_fence_after();
   pdl_wait();
   const uint32_t tmem = tmem_slot;
-  const int nk = (a.k + 63) >> 6;
+  const int ns = (a.k + 127) >> 7;
   const int mine = ((int)blockIdx.x < tiles ? (tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0);
 
   if (warp == 0) {
@@ -574,16 +676,20 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         ok = mbar_wait(smem_u32(&acc_empty[acc]), ((n >> 1) & 1) ^ 1, lim);
         if (!ok) break;
         tc_fence_after();
-        for (int i = 0; i < nk; ++i) {
+        for (int i = 0; i < ns; ++i) {
           ok = mbar_wait(smem_u32(&full[stage]), phase, lim);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE));
-          const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            tc_mma_f16(tmem + (uint32_t)(acc * BN), ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc,
-                       i > 0 || kk > 0);
+          for (int h = 0; h < 2; ++h) {
+            if (i * 128 + h * 64 >= a.k) break;
+            const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE + h * Cfg::HALF));
+            const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_f16(tmem + (uint32_t)(acc * BN), ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc,
+                         i > 0 || h > 0 || kk > 0);
+          }
           tc_commit(smem_u32(&empty[stage]));
           if (++stage == Cfg::STAGES) {
             stage = 0;
@@ -600,7 +706,6 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   } else if (warp <= 4) {
     const int quad = warp & 3, et = tid - 32;
     const uint32_t stage_w = smem_u32(staging + (warp - 1) * 4096);
-    const bool vec = (a.n & 7) == 0;
     for (int n = 0; n < mine; ++n) {
       const int acc = n & 1, tile = (int)blockIdx.x + n * (int)gridDim.x;
       const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
@@ -618,88 +723,25 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       }
       tc_fence_after();
       const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
-#pragma unroll 1
-      for (int c = 0; c < BN; c += 64) {
-        if (q0 + c >= a.n) break;
-#pragma unroll
-        for (int h = 0; h < 64; h += 32) {
-          uint32_t r[32];
-          tmem_ld16(tacc + (uint32_t)(c + h), r);
-          tmem_ld16(tacc + (uint32_t)(c + h + 16), r + 16);
-          tmem_ld_wait();
-          const float4* sb = reinterpret_cast<const float4*>(swb + acc * BN + c + h);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t o[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float4 f = sb[j * 4 + q];  // two channels
-              o[q] = f2h2(fmaf(__uint_as_float(r[8 * j + 2 * q]), sx * f.x, f.y),
-                          fmaf(__uint_as_float(r[8 * j + 2 * q + 1]), sx * f.z, f.w));
-            }
-            st_shared_v4(stage_w + (uint32_t)(lane * 128 + (((h / 8 + j) ^ (lane & 7)) << 4)),
-                         make_uint4(o[0], o[1], o[2], o[3]));
-          }
-        }
-        __syncwarp();
-        // 32 rows of 64 channels, whole 128-byte rows at a time
-        const int left = a.n - q0 - c, r0 = p0 + quad * 32;
-        if (vec) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int rr = i * 4 + (lane >> 3), ch = lane & 7;
-            uint4 v;
-            ld_shared_v4(stage_w + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)), v);
-            if (r0 + rr < a.m && ch * 8 < left)
-              *reinterpret_cast<uint4*>(a.y + (long long)(r0 + rr) * a.n + q0 + c + ch * 8) = v;
-          }
-        } else {
-          const uint16_t* sp = reinterpret_cast<const uint16_t*>(staging + (warp - 1) * 4096);
-          for (int i = 0; i < 64; ++i) {
-            const int rr = i >> 1, e = (i & 1) * 32 + lane;
-            if (r0 + rr < a.m && e < left)
-              a.y[(long long)(r0 + rr) * a.n + q0 + c + e] = sp[rr * 64 + (((e >> 3) ^ (rr & 7)) << 3) + (e & 7)];
-          }
-        }
-        __syncwarp();
-      }
+      store_tile<BN>(a, tacc, swb + acc * BN, stage_w, staging + (warp - 1) * 4096, p0 + quad * 32, q0, sx, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
     }
   } else {
-    const int ct = tid - 160, c = ct & 3;
-    const int8_t* base[Cfg::U];
-    bool live[Cfg::U];
-    auto place = [&](int n) {  // this thread's rows in the n-th tile
-      const int tile = (int)blockIdx.x + n * (int)gridDim.x;
-      const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
-#pragma unroll
-      for (int i = 0; i < Cfg::U; ++i) {
-        const int row = (i < 2 ? p0 + i * 64 : q0 + (i - 2) * 64) + (ct >> 2);
-        live[i] = n < mine && row < (i < 2 ? a.m : a.n);
-        base[i] = (i < 2 ? a.x : a.w) + (long long)(live[i] ? row : 0) * a.k;
-      }
-    };
+    const int ct = tid - 160;
+    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a, ct, (int)blockIdx.x, (int)gridDim.x, mine, ns, q_tiles, 128, BN, 0, 0);
     uint4 raw[Cfg::DIST][Cfg::U];
-    int fn = 0, fk = 0;  // the next K-block to fetch
-    place(0);
-    auto fetch = [&](uint4* dst) {
-      const int at = fk * 64 + c * 16;
 #pragma unroll
-      for (int u = 0; u < Cfg::U; ++u)
-        dst[u] = live[u] ? load16<ALIGNED>(base[u], at, a.k) : make_uint4(0, 0, 0, 0);
-      if (++fk == nk) {
-        fk = 0;
-        place(++fn);
-      }
-    };
+    for (int d = 0; d < Cfg::DIST; ++d) {
 #pragma unroll
-    for (int d = 0; d < Cfg::DIST; ++d) fetch(raw[d]);
+      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, raw[d][u]);
+      feed.next();
+    }
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    const long long total = (long long)mine * nk;
+    const long long total = (long long)mine * ns;
     for (long long i = 0; ok && i < total; i += Cfg::DIST) {
 #pragma unroll
       for (int d = 0; d < Cfg::DIST; ++d) {
@@ -709,14 +751,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           atomicCAS(status, 0, -7);
           break;
         }
-        const uint32_t sp = smem_u32(smem + stage * Cfg::STAGE), sq = sp + 128 * 128;
-#pragma unroll
-        for (int u = 0; u < Cfg::U; ++u)
-          put16(u < 2 ? sp : sq, (ct >> 2) + (u < 2 ? u : u - 2) * 64, c, raw[d][u]);
-        fence_proxy_async_smem();
-        __syncwarp();
+        feed.convert(raw[d], smem_u32(smem + stage * Cfg::STAGE + ((ct >> 2) & 1) * Cfg::HALF));
         if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
-        fetch(raw[d]);
         if (++stage == Cfg::STAGES) {
           stage = 0;
           phase ^= 1;
@@ -729,6 +765,193 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   if (warp == 0 && drained) {
     tc_fence_after();
     tmem_dealloc(tmem, 2 * BN);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The same for many channels too: tiles of 256 rows by 256 channels, made by a
+// pair of CTAs (cta_group::2).  Each CTA converts 128 rows of x and 128 of w per
+// tile where a single one's 128 x 256 tile takes 128 and 256: a third less to
+// load, to widen and to store in shared memory for each MMA, which is what bound
+// that one.
+//
+// The MMAs read both CTAs' tiles, so the leading CTA has to know when the other
+// one's are complete.  An arrival there that releases this CTA's writes takes
+// about 1000 clocks, so three warps of the other CTA pass the stages on, a stage
+// each, and the pipeline is deep enough to hide them.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kPairThreads = 32 * 16;  // MMA, four storing warps, eight converting warps, three relaying ones
+
+struct PairCfg {
+  static constexpr int HALF = 256 * 128;
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int STAGES = 3;
+  static constexpr int DIST = 2;
+  static constexpr int UP = 4, U = 8;
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * 4096 + 2 * 256 * 8;
+};
+
+}  // namespace
+
+template <bool ALIGNED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    k_linear_i8_pair(const LinearI8 a, int q_tiles, int tiles, int* status, unsigned long long lim) {
+  using Cfg = PairCfg;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* staging = smem + Cfg::STAGES * Cfg::STAGE;           // 4 KB a storing warp
+  float2* swb = reinterpret_cast<float2*>(staging + 4 * 4096);  // [2][256] scale and bias of a channel
+  __shared__ uint64_t full[Cfg::STAGES], empty[Cfg::STAGES], acc_full[2], acc_empty[2], last;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int drained;
+  const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)cluster_rank();
+  if (tid == 0) {
+    for (int i = 0; i < Cfg::STAGES; ++i) {
+      mbar_init(smem_u32(&full[i]), rank == 0 ? 9 : 8);  // the converting warps, and the other CTA's relay
+      mbar_init(smem_u32(&empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&acc_full[i]), 1);
+      mbar_init(smem_u32(&acc_empty[i]), 8);  // (the leading CTA's) both CTAs' storing warps
+    }
+    mbar_init(smem_u32(&last), 1);
+    drained = 1;
+    fence_mbar_init();
+  }
+  if (warp == 0) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = tmem_slot;
+  const int ns = (a.k + 127) >> 7;
+  const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+  const int mine = pair < tiles ? (tiles - 1 - pair) / pairs + 1 : 0;
+
+  if (warp == 0) {
+    if (rank == 0 && elect_one()) {
+      const uint64_t desc = smem_desc(0, 16, 1024, 2);
+      const uint32_t idesc = idesc_f16(256, 256, false, false, true);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int n = 0; n < mine && ok; ++n) {
+        const int acc = n & 1;
+        ok = mbar_wait_cluster(smem_u32(&acc_empty[acc]), ((n >> 1) & 1) ^ 1, lim);
+        if (!ok) break;
+        tc_fence_after();
+        for (int i = 0; i < ns; ++i) {
+          ok = mbar_wait_cluster(smem_u32(&full[stage]), phase, lim);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (i * 128 + h * 64 >= a.k) break;
+            const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE + h * Cfg::HALF));
+            const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_f16_pair(tmem + (uint32_t)(acc * 256), ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc,
+                              i > 0 || h > 0 || kk > 0);
+          }
+          tc_commit_pair(smem_u32(&empty[stage]));
+          if (++stage == Cfg::STAGES) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        if (ok) tc_commit_pair(smem_u32(&acc_full[acc]));
+      }
+      if (!ok) atomicCAS(status, 0, -7);  // PF16_ERR_TIMEOUT
+      tc_commit_pair_here(smem_u32(&last));  // nothing runs in either CTA's TMEM when it is released
+      if (!mbar_wait(smem_u32(&last), 0, lim)) {
+        drained = 0;
+        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_rank(smem_u32(&drained), 1)), "r"(0) : "memory");
+      }
+    }
+    __syncwarp();
+  } else if (warp <= 4) {
+    const int quad = warp & 3, et = tid - 32;
+    const uint32_t stage_w = smem_u32(staging + (warp - 1) * 4096);
+    const uint32_t far_acc = map_rank(smem_u32(&acc_empty[0]), 0);
+    for (int n = 0; n < mine; ++n) {
+      const int acc = n & 1, tile = pair + n * pairs;
+      const int r0 = (tile / q_tiles) * 256 + rank * 128 + quad * 32, q0 = (tile % q_tiles) * 256;
+      // this tile's channel scales and biases; the other buffer may still be read
+      for (int j = et; j < 256; j += 128) {
+        const int q = q0 + j;
+        swb[acc * 256 + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const float sx = r0 + lane < a.m ? a.sx[r0 + lane] : 0.f;
+      if (!mbar_wait_cluster(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
+        atomicCAS(status, 0, -7);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256);
+      store_tile<256>(a, tacc, swb + acc * 256, stage_w, staging + (warp - 1) * 4096, r0, q0, sx, lane);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
+    }
+  } else if (warp <= 12) {
+    const int ct = tid - 160;
+    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a, ct, pair, pairs, mine, ns, q_tiles, 256, 256, rank * 128, rank * 128);
+    uint4 raw[Cfg::DIST][Cfg::U];
+#pragma unroll
+    for (int d = 0; d < Cfg::DIST; ++d) {
+#pragma unroll
+      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, raw[d][u]);
+      feed.next();
+    }
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const long long total = (long long)mine * ns;
+    for (long long i = 0; ok && i < total; i += Cfg::DIST) {
+#pragma unroll
+      for (int d = 0; d < Cfg::DIST; ++d) {
+        if (i + d >= total) break;
+        ok = mbar_wait_cluster(smem_u32(&empty[stage]), phase ^ 1, 2 * lim);
+        if (!ok) {
+          atomicCAS(status, 0, -7);
+          break;
+        }
+        feed.convert(raw[d], smem_u32(smem + stage * Cfg::STAGE + ((ct >> 2) & 1) * Cfg::HALF));
+        if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
+        if (++stage == Cfg::STAGES) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+    }
+  } else {
+    if (rank == 1 && elect_one()) {
+      const int stage = warp - 13;  // this warp's (Cfg::STAGES is the number of these warps)
+      const uint32_t far = map_rank(smem_u32(&full[stage]), 0);
+      uint32_t phase = 0;
+      for (long long i = stage; i < (long long)mine * ns; i += Cfg::STAGES, phase ^= 1) {
+        if (!mbar_wait(smem_u32(&full[stage]), phase, 2 * lim)) {
+          atomicCAS(status, 0, -7);
+          break;
+        }
+        mbar_arrive_cluster(far);
+      }
+    }
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // neither CTA leaves while the other may still reach into it
+  if (warp == 0 && drained) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
   }
 }
 
@@ -785,6 +1008,20 @@ cudaError_t linear_big(const LinearI8& a, int sms, int* status, cudaStream_t s) 
   return (a.k & 15) == 0 ? linear_big_al<BN, true>(a, sms, status, s) : linear_big_al<BN, false>(a, sms, status, s);
 }
 
+template <bool ALIGNED>
+cudaError_t linear_pair_al(const LinearI8& a, int sms, int* status, cudaStream_t s) {
+  auto kernel = k_linear_i8_pair<ALIGNED>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg::SMEM);
+  if (e != cudaSuccess) return e;
+  const int q_tiles = (a.n + 255) / 256;
+  const long long tiles = (long long)((a.m + 255) / 256) * q_tiles;
+  if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
+  const int pairs = tiles < sms / 2 ? (int)tiles : sms / 2;
+  e = launch_pdl(kernel, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), PairCfg::SMEM, s, a, q_tiles, (int)tiles,
+                 status, 4000000000ull);
+  return e == cudaSuccess ? counted_launches(1) : e;
+}
+
 template <int MT>
 cudaError_t linear_rows(const LinearI8& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)((a.m + MT - 1) / MT));
@@ -819,7 +1056,8 @@ cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream
       if (splits > 1) return linear_al<64, false>(a, splits, status, s);
       return linear_big<64>(a, sms, status, s);
     case 128: return linear_big<128>(a, sms, status, s);
-    default: return linear_big<256>(a, sms, status, s);
+    default:
+      return (a.k & 15) == 0 ? linear_pair_al<true>(a, sms, status, s) : linear_pair_al<false>(a, sms, status, s);
   }
 }
 

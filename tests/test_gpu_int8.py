@@ -128,7 +128,16 @@ def test_linear(m, n, k):
         check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 64, 1024), (6, 130, 1024), (130, 70, 1024), (20, 260, 1024), (300, 300, 1024)])
+# many tiles: every CTA or pair of them has several, the last ones ragged in all three sizes
+@pytest.mark.parametrize("m,n,k", [(5000, 1000, 208), (5001, 1003, 65), (20000, 264, 64), (9000, 700, 513),
+                                   (40000, 128, 16), (39999, 100, 147), (50000, 64, 160), (50001, 33, 40)])
+def test_linear_many_tiles(m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    x, sx, w, sw, b = operands(rng, m, n, k)
+    check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
+
+
+@pytest.mark.parametrize("m,n,k", [(5000, 1000, 1024), (40000, 128, 1024), (1, 64, 1024), (6, 130, 1024), (130, 70, 1024), (20, 260, 1024), (300, 300, 1024)])
 def test_linear_sums_are_exact(m, n, k):
     """Scales of one: sums up to 1024 * 128^2 = 2^24 come out as binary16 rounds the exact integers
     (scaled so that none overflows)."""
