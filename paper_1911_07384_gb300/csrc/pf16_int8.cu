@@ -512,19 +512,20 @@ template <int BN>
 struct BigCfg {
   static constexpr int HALF = (128 + BN) * 128;  // one K-block: P's tile, then Q's
   static constexpr int STAGE = 2 * HALF;
-  static constexpr int STAGES = BN >= 256 ? 2 : BN >= 128 ? 3 : 4;
+  static constexpr int STAGES = BN >= 128 ? 3 : 4;
   static constexpr int DIST = BN >= 128 ? 2 : 3;  // stages of raw bytes in registers
   static constexpr int UP = 4, U = UP + BN / 32;  // 16-byte units of P, of both, that a thread loads per stage
   static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * 4096 + 2 * BN * 8;
 };
 
-// A converting thread's share of the operands: unit u of a stage is bytes 16 (ct & 7) of row (ct >> 3) + 32 u of
-// P, or of row (ct >> 3) + 32 (u - UP) of Q.  The raw bytes of DIST stages are in registers.
+// A converting thread's share of the operands: unit u of a stage is bytes 16 (ct & 7) of row `row` + 32 u of
+// P, or of row `row` + 32 (u - UP) of Q.  The lanes of a row's second 64 bytes, whose K-block's tile lies a multiple
+// of 128 bytes away, take the neighbouring row's instead: its swizzle puts them in the other banks.  The raw bytes of DIST stages are in registers.
 // Tile t of this CTA has its rows of P from p0 + ..., given by the caller (`first`, as rows of x and w).
 template <int UP, int U, bool ALIGNED>
 struct Feed {
   const LinearI8& a;
-  const int ct, tiles, ns, step_tile, q_tiles, pm, qm, pofs, qofs;
+  const int ct, row, tiles, ns, step_tile, q_tiles, pm, qm, pofs, qofs;
   int tile, n, s;  // of the next stage to fetch: the tile, how many tiles before it, the stage in it
   const int8_t *pb, *qb;
   int pl, ql;      // rows from this thread's first to the end
@@ -534,12 +535,12 @@ struct Feed {
   // of w
   __device__ __forceinline__ Feed(const LinearI8& a_, int ct_, int first, int step_tile_, int tiles_, int ns_,
                                   int q_tiles_, int pm_, int qm_, int pofs_, int qofs_)
-      : a(a_), ct(ct_), tiles(tiles_), ns(ns_), step_tile(step_tile_), q_tiles(q_tiles_), pm(pm_), qm(qm_),
+      : a(a_), ct(ct_), row((ct_ >> 3) ^ ((ct_ >> 2) & 1)), tiles(tiles_), ns(ns_), step_tile(step_tile_), q_tiles(q_tiles_), pm(pm_), qm(qm_),
         pofs(pofs_), qofs(qofs_), tile(first), n(0), s(0), step(32ll * a_.k) {
     place();
   }
   __device__ __forceinline__ void place() {
-    const int pr = (tile / q_tiles) * pm + pofs + (ct >> 3), qr = (tile % q_tiles) * qm + qofs + (ct >> 3);
+    const int pr = (tile / q_tiles) * pm + pofs + row, qr = (tile % q_tiles) * qm + qofs + row;
     pl = n < tiles ? a.m - pr : 0;
     ql = n < tiles ? a.n - qr : 0;
     pb = a.x + (pl > 0 ? (long long)pr * a.k : 0);
@@ -563,7 +564,7 @@ struct Feed {
   __device__ __forceinline__ void convert(uint4 (&raw)[U], uint32_t half) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      put16(half + (u < UP ? 0 : 128 * 128), (ct >> 3) + (u < UP ? u : u - UP) * 32, ct & 3, raw[u]);
+      put16(half + (u < UP ? 0 : 128 * 128), row + (u < UP ? u : u - UP) * 32, ct & 3, raw[u]);
       fetch(u, raw[u]);
     }
     next();
@@ -572,32 +573,52 @@ struct Feed {
   }
 };
 
-// One storing warp's 32 rows (from r0 on) of a tile of BN channels (from q0 on): scaled, rounded, and
-// through 4 KB of shared memory into whole rows of 64 channels.
+// 16 rows of TMEM by 32 columns as fragments of 8 x 8: thread t has columns 2 (t & 3) and + 1 of each eight, of
+// row t >> 2 (r[4 g], r[4 g + 1]) and of row 8 + (t >> 2).
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// four 8 x 8 binary16 matrices, thread t's row address and its pair of each
+__device__ __forceinline__ void st_matrix4(uint32_t row, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(row), "r"(a), "r"(b), "r"(c),
+               "r"(d)
+               : "memory");
+}
+
+// One storing warp's 32 rows (from r0 on) of a tile of BN channels (from q0 on): scaled, rounded, and through
+// 4 KB of shared memory into whole rows of 64 channels.  swb: the channels' scales and biases; sx: those of rows
+// r0 + 8 i + (lane >> 2).  The accumulators come as 8 x 8 fragments, in which a thread has a quarter of the
+// channels of four rows: with all channels of one row it read four times as many scales, whose loads took a
+// quarter of the kernel's time at 64 values of K.
 template <int BN>
-__device__ __forceinline__ void store_tile(const LinearI8& a, uint32_t tacc, const float2* swb, uint32_t stage_w,
-                                           const uint8_t* stage_p, int r0, int q0, float sx, int lane) {
+__device__ __forceinline__ void store_tile(const LinearI8& a, uint32_t tacc, const float2* swb, uint8_t* stage_p,
+                                           int r0, int q0, const float (&sx)[4], int lane) {
+  const uint32_t stage_w = smem_u32(stage_p) + (uint32_t)lane * 128u;
 #pragma unroll 1
   for (int c = 0; c < BN; c += 64) {
     if (q0 + c >= a.n) break;
 #pragma unroll
-    for (int h = 0; h < 64; h += 32) {
-      uint32_t r[32];
-      tmem_ld16(tacc + (uint32_t)(c + h), r);
-      tmem_ld16(tacc + (uint32_t)(c + h + 16), r + 16);
+    for (int h = 0; h < 2; ++h) {
+      uint32_t u[16], v[16];
+      tmem_ld_frag(tacc + (uint32_t)(c + h * 32), u);
+      tmem_ld_frag(tacc + (16u << 16) + (uint32_t)(c + h * 32), v);
       tmem_ld_wait();
-      const float4* sb = reinterpret_cast<const float4*>(swb + c + h);
+      const float4* sb = reinterpret_cast<const float4*>(swb + c + h * 32) + (lane & 3);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int g = 0; g < 4; ++g) {
+        const float4 f = sb[g * 4];  // two channels
         uint32_t o[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 f = sb[j * 4 + q];  // two channels
-          o[q] = f2h2(fmaf(__uint_as_float(r[8 * j + 2 * q]), sx * f.x, f.y),
-                      fmaf(__uint_as_float(r[8 * j + 2 * q + 1]), sx * f.z, f.w));
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t* r = (i < 2 ? u : v) + 4 * g + 2 * (i & 1);
+          o[i] = f2h2(fmaf(__uint_as_float(r[0]), sx[i] * f.x, f.y), fmaf(__uint_as_float(r[1]), sx[i] * f.z, f.w));
         }
-        st_shared_v4(stage_w + (uint32_t)(lane * 128 + (((h / 8 + j) ^ (lane & 7)) << 4)),
-                     make_uint4(o[0], o[1], o[2], o[3]));
+        st_matrix4(stage_w + (uint32_t)(((h * 4 + g) ^ (lane & 7)) << 4), o[0], o[1], o[2], o[3]);
       }
     }
     __syncwarp();
@@ -607,10 +628,10 @@ __device__ __forceinline__ void store_tile(const LinearI8& a, uint32_t tacc, con
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int rr = i * 4 + (lane >> 3), ch = lane & 7;
-        uint4 v;
-        ld_shared_v4(stage_w + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)), v);
+        uint4 y;
+        ld_shared_v4(smem_u32(stage_p) + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)), y);
         if (r0 + rr < a.m && ch * 8 < left)
-          *reinterpret_cast<uint4*>(a.y + (long long)(r0 + rr) * a.n + q0 + c + ch * 8) = v;
+          *reinterpret_cast<uint4*>(a.y + (long long)(r0 + rr) * a.n + q0 + c + ch * 8) = y;
       }
     } else {
       const uint16_t* sp = reinterpret_cast<const uint16_t*>(stage_p);
@@ -705,7 +726,6 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     __syncwarp();
   } else if (warp <= 4) {
     const int quad = warp & 3, et = tid - 32;
-    const uint32_t stage_w = smem_u32(staging + (warp - 1) * 4096);
     for (int n = 0; n < mine; ++n) {
       const int acc = n & 1, tile = (int)blockIdx.x + n * (int)gridDim.x;
       const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
@@ -715,15 +735,19 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         swb[acc * BN + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
       }
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      const int row = p0 + quad * 32 + lane;
-      const float sx = row < a.m ? a.sx[row] : 0.f;
+      float sx[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = p0 + quad * 32 + i * 8 + (lane >> 2);
+        sx[i] = row < a.m ? a.sx[row] : 0.f;
+      }
       if (!mbar_wait(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
         atomicCAS(status, 0, -7);
         break;
       }
       tc_fence_after();
       const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
-      store_tile<BN>(a, tacc, swb + acc * BN, stage_w, staging + (warp - 1) * 4096, p0 + quad * 32, q0, sx, lane);
+      store_tile<BN>(a, tacc, swb + acc * BN, staging + (warp - 1) * 4096, p0 + quad * 32, q0, sx, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
@@ -877,7 +901,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     __syncwarp();
   } else if (warp <= 4) {
     const int quad = warp & 3, et = tid - 32;
-    const uint32_t stage_w = smem_u32(staging + (warp - 1) * 4096);
     const uint32_t far_acc = map_rank(smem_u32(&acc_empty[0]), 0);
     for (int n = 0; n < mine; ++n) {
       const int acc = n & 1, tile = pair + n * pairs;
@@ -888,14 +911,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         swb[acc * 256 + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
       }
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      const float sx = r0 + lane < a.m ? a.sx[r0 + lane] : 0.f;
+      float sx[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = r0 + i * 8 + (lane >> 2);
+        sx[i] = row < a.m ? a.sx[row] : 0.f;
+      }
       if (!mbar_wait_cluster(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
         atomicCAS(status, 0, -7);
         break;
       }
       tc_fence_after();
       const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256);
-      store_tile<256>(a, tacc, swb + acc * 256, stage_w, staging + (warp - 1) * 4096, r0, q0, sx, lane);
+      store_tile<256>(a, tacc, swb + acc * 256, staging + (warp - 1) * 4096, r0, q0, sx, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
