@@ -573,6 +573,27 @@ struct Feed {
   }
 };
 
+// What a storing thread reads of a tile before it stores it: the scales of its four rows (r0 + 8 i + (lane >> 2)) and
+// the scales and biases of two channels, its share of all storing threads'.  Fetched a tile ahead.
+struct TileScales {
+  float sx[4];
+  float4 ch;
+  template <int BN>
+  __device__ __forceinline__ void fetch(const LinearI8& a, int r0, int q0, int et) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = r0 + i * 8 + ((et & 31) >> 2);
+      sx[i] = row < a.m ? __ldg(a.sx + row) : 0.f;
+    }
+    const int q = q0 + 2 * et;
+    const bool in0 = 2 * et < BN && q < a.n, in1 = 2 * et < BN && q + 1 < a.n;
+    ch.x = in0 ? __ldg(a.sw + q) : 0.f;
+    ch.z = in1 ? __ldg(a.sw + q + 1) : 0.f;
+    ch.y = in0 && a.bias ? h2f(__ldg(a.bias + q)) : 0.f;
+    ch.w = in1 && a.bias ? h2f(__ldg(a.bias + q + 1)) : 0.f;
+  }
+};
+
 // 16 rows of TMEM by 32 columns as fragments of 8 x 8: thread t has columns 2 (t & 3) and + 1 of each eight, of
 // row t >> 2 (r[4 g], r[4 g + 1]) and of row 8 + (t >> 2).
 __device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t* r) {
@@ -726,21 +747,19 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     __syncwarp();
   } else if (warp <= 4) {
     const int quad = warp & 3, et = tid - 32;
+    TileScales next;
+    auto fetch = [&](int n) {
+      const int tile = (int)blockIdx.x + n * (int)gridDim.x;
+      if (n < mine) next.fetch<BN>(a, (tile / q_tiles) * 128 + quad * 32, (tile % q_tiles) * BN, et);
+    };
+    fetch(0);
     for (int n = 0; n < mine; ++n) {
       const int acc = n & 1, tile = (int)blockIdx.x + n * (int)gridDim.x;
       const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
-      // this tile's channel scales and biases; the other buffer may still be read
-      for (int j = et; j < BN; j += 128) {
-        const int q = q0 + j;
-        swb[acc * BN + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
-      }
+      if (2 * et < BN) reinterpret_cast<float4*>(swb + acc * BN)[et] = next.ch;  // (the other buffer may still be read)
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      float sx[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = p0 + quad * 32 + i * 8 + (lane >> 2);
-        sx[i] = row < a.m ? a.sx[row] : 0.f;
-      }
+      const float sx[4] = {next.sx[0], next.sx[1], next.sx[2], next.sx[3]};
+      fetch(n + 1);
       if (!mbar_wait(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
         atomicCAS(status, 0, -7);
         break;
@@ -902,21 +921,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   } else if (warp <= 4) {
     const int quad = warp & 3, et = tid - 32;
     const uint32_t far_acc = map_rank(smem_u32(&acc_empty[0]), 0);
+    TileScales next;
+    auto fetch = [&](int n) {
+      const int tile = pair + n * pairs;
+      if (n < mine) next.fetch<256>(a, (tile / q_tiles) * 256 + rank * 128 + quad * 32, (tile % q_tiles) * 256, et);
+    };
+    fetch(0);
     for (int n = 0; n < mine; ++n) {
       const int acc = n & 1, tile = pair + n * pairs;
       const int r0 = (tile / q_tiles) * 256 + rank * 128 + quad * 32, q0 = (tile % q_tiles) * 256;
-      // this tile's channel scales and biases; the other buffer may still be read
-      for (int j = et; j < 256; j += 128) {
-        const int q = q0 + j;
-        swb[acc * 256 + j] = q < a.n ? make_float2(a.sw[q], a.bias ? h2f(a.bias[q]) : 0.f) : make_float2(0.f, 0.f);
-      }
+      reinterpret_cast<float4*>(swb + acc * 256)[et] = next.ch;  // (the other buffer may still be read)
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      float sx[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = r0 + i * 8 + (lane >> 2);
-        sx[i] = row < a.m ? a.sx[row] : 0.f;
-      }
+      const float sx[4] = {next.sx[0], next.sx[1], next.sx[2], next.sx[3]};
+      fetch(n + 1);
       if (!mbar_wait_cluster(smem_u32(&acc_full[acc]), (n >> 1) & 1, 2 * lim)) {
         atomicCAS(status, 0, -7);
         break;
