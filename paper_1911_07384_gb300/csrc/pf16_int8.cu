@@ -173,9 +173,10 @@ cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long 
 }
 
 // ---------------------------------------------------------------------------
-// The product for a few rows of x: each warp takes one output channel, its
-// lanes 16 bytes of the weight row at a time, and multiplies them with the MT
-// rows of x by dp4a (exact 32-bit sums).  Bound by the weight's bytes, read once.
+// The product for a few rows of x: each warp takes one output channel of one row, its
+// lanes 16 bytes of the weight row at a time, by dp4a (exact 32-bit sums).  Bound
+// by the weight's bytes: from HBM for one row of x (8192 x 8192: 5.3 TB/s), from
+// the L2, which the rows' CTAs share, for several (12.5 TB/s).
 // ---------------------------------------------------------------------------
 namespace {
 
@@ -184,6 +185,11 @@ namespace {
 template <bool ALIGNED>
 __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
   if (ALIGNED) return c < k ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+  if ((k & 7) == 0) {
+    const uint2* p = reinterpret_cast<const uint2*>(row + c);
+    const uint2 z = make_uint2(0, 0), lo = c < k ? __ldg(p) : z, hi = c + 8 < k ? __ldg(p + 1) : z;
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+  }
   // Whole words around the 16 bytes while they end inside the row (they start in the
   // array: rows before this one, or the array's aligned start, precede it).
   const int lead = (int)(reinterpret_cast<uintptr_t>(row + c) & 3u);
@@ -203,38 +209,25 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
 
 }  // namespace
 
-template <int MT, bool ALIGNED>
+template <bool ALIGNED>
 __global__ void __launch_bounds__(256) k_linear_i8_rows(const LinearI8 a) {
   pdl_wait();
   const int lane = (int)threadIdx.x & 31;
-  const int j = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5);
-  const int m0 = (int)blockIdx.y * MT;
+  const int j = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), i = (int)blockIdx.y;
   if (j >= a.n) return;
   const int8_t* w = a.w + (long long)j * a.k;
-  int acc[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = 0;
+  const int8_t* x = a.x + (long long)i * a.k;
+  int acc = 0;
 #pragma unroll 2
   for (int c = lane * 16; c < a.k; c += 512) {
-    const uint4 wv = load16<ALIGNED>(w, c, a.k);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if (m0 + i < a.m) {
-        const uint4 xv = load16<ALIGNED>(a.x + (long long)(m0 + i) * a.k, c, a.k);
-        acc[i] = __dp4a((int)wv.x, (int)xv.x, acc[i]);
-        acc[i] = __dp4a((int)wv.y, (int)xv.y, acc[i]);
-        acc[i] = __dp4a((int)wv.z, (int)xv.z, acc[i]);
-        acc[i] = __dp4a((int)wv.w, (int)xv.w, acc[i]);
-      }
-    }
+    const uint4 wv = load16<ALIGNED>(w, c, a.k), xv = load16<ALIGNED>(x, c, a.k);
+    acc = __dp4a((int)wv.x, (int)xv.x, acc);
+    acc = __dp4a((int)wv.y, (int)xv.y, acc);
+    acc = __dp4a((int)wv.z, (int)xv.z, acc);
+    acc = __dp4a((int)wv.w, (int)xv.w, acc);
   }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int s = __reduce_add_sync(0xffffffffu, acc[i]);
-    if (lane == 0 && m0 + i < a.m)
-      a.y[(long long)(m0 + i) * a.n + j] =
-          f2h(fmaf((float)s, a.sx[m0 + i] * a.sw[j], a.bias ? h2f(a.bias[j]) : 0.f));
-  }
+  const int s = __reduce_add_sync(0xffffffffu, acc);
+  if (lane == 0) a.y[(long long)i * a.n + j] = f2h(fmaf((float)s, a.sx[i] * a.sw[j], a.bias ? h2f(a.bias[j]) : 0.f));
 }
 
 // ---------------------------------------------------------------------------
@@ -261,9 +254,9 @@ constexpr int kI8Threads = 288;  // eight converting (then storing) warps, one M
 template <int BN>
 struct I8Cfg {
   static constexpr int STAGE = (128 + BN) * 128;
-  static constexpr int STAGES = BN >= 256 ? 4 : BN >= 128 ? 3 : 4;
-  static constexpr int DIST = BN >= 128 ? 2 : 4;  // K-blocks of raw bytes in registers ahead of the conversion
-  static constexpr int CTAS = BN >= 256 ? 1 : 2;
+  static constexpr int STAGES = 4;
+  static constexpr int DIST = 4;  // K-blocks of raw bytes in registers ahead of the conversion
+  static constexpr int CTAS = 2;
   static constexpr int SMEM = 1024 + STAGES * STAGE;
   static constexpr int TMEM = BN < 32 ? 32 : BN;
   static constexpr int UQ = (BN * 4 + 255) / 256;  // 16-byte units of Q a thread loads per K-block
@@ -1067,42 +1060,76 @@ cudaError_t linear_pair_al(const LinearI8& a, int sms, int* status, cudaStream_t
   return e == cudaSuccess ? counted_launches(1) : e;
 }
 
-template <int MT>
+cudaError_t linear_pair(const LinearI8& a, int sms, int* status, cudaStream_t s) {
+  return (a.k & 15) == 0 ? linear_pair_al<true>(a, sms, status, s) : linear_pair_al<false>(a, sms, status, s);
+}
+
 cudaError_t linear_rows(const LinearI8& a, cudaStream_t s) {
-  const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)((a.m + MT - 1) / MT));
-  const cudaError_t e = (a.k & 15) == 0 ? launch_pdl(k_linear_i8_rows<MT, true>, grid, dim3(256), 0, s, a)
-                                        : launch_pdl(k_linear_i8_rows<MT, false>, grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((a.n + 7) / 8), (unsigned)a.m);
+  const cudaError_t e = (a.k & 15) == 0 ? launch_pdl(k_linear_i8_rows<true>, grid, dim3(256), 0, s, a)
+                                        : launch_pdl(k_linear_i8_rows<false>, grid, dim3(256), 0, s, a);
   return e == cudaSuccess ? counted_launches(1) : e;
+}
+
+// The variants' times in microseconds, as measured and interpolated, from the sizes alone.
+//
+// One warp an element against the tensor cores with 128 channels in an MMA's rows (m n k: us, us):
+//   8 1000 2048: 2.8, 6.2    6 2048 2048: 3.9, 6.7    12 4096 1024: 5.8, 5.9    2 8192 8192: 17.4, 20.5
+//   4 8192 8192: 26.7, 20.7  8 8192 8192: 42.8, 21.0
+bool rows_faster(const LinearI8& a) {
+  const double bytes = (double)a.n * a.k;
+  return a.m <= 32 && 1.8 + a.m * bytes / 12.5e6 < 5.5 + bytes / 4.4e6;
+}
+
+enum Variant { V_SPLIT2, V_SPLIT4, V_BIG64, V_BIG128, V_PAIR };
+// Many rows of x: a launch, then rounds of one tile for each CTA (or pair), each of stages of 128
+// values of K and the part of its storing that nothing hides.  Split K: CTAs of 128 x 64 tiles, two
+// an SM, bound by one CTA's K-blocks or by what an SM's CTAs have together.
+//   m n k              split 2, 4   64 wide  128 wide  pairs
+//   512 1000 2048       10.5 11.1     12.8     15.7     19.4
+//   4096 128 2048       11.4 11.6     14.3     17.3     18.7
+//   1000 1000 1024      11.3 15.7      8.2     10.0     13.6
+//   128 8192 8192       56.7           43.6    55.4
+//   4096 512 512        16.4 24.5      8.5      6.9     10.5
+//   512 4096 4096       54.3 62.7     41.1     28.6     35.4
+//   2048 2048 2048      62.7 74.4     41.3     29.3     21.9
+//   12544 2048 512       157  257     58.1     43.8     39.1
+Variant pick(const LinearI8& a, int sms) {
+  auto up = [](long long x, long long y) { return (double)((x + y - 1) / y); };
+  const double ns = up(a.k, 128), kbs = up(a.k, 64), p = up(a.m, 128);
+  const double t64 = p * up(a.n, 64), t128 = p * up(a.n, 128), t256 = up(a.m, 256) * up(a.n, 256);
+  auto rounds = [&](double tiles, int slots) { return up((long long)tiles, slots); };
+  auto split = [&](int s) {
+    const double own = kbs / s * 0.4, sm = t64 * kbs / sms * 0.45;
+    return t64 * s > 2 * sms ? 1e30 : 4.5 + (own > sm ? own : sm);
+  };
+  const double us[] = {split(2), split(4), 3 + rounds(t64, sms) * (0.63 * ns + 0.6),
+                       3 + rounds(t128, sms) * (0.77 * ns + 0.8), 5 + rounds(t256, sms / 2) * (0.85 * ns + 1.6)};
+  int best = V_BIG64;
+  for (int v = 0; v < 5; ++v)
+    if (us[v] < us[best]) best = v;
+  return (Variant)best;
 }
 
 }  // namespace
 
 cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s) {
-  if (a.m == 1) return linear_rows<1>(a, s);
-  if (a.m == 2) return linear_rows<2>(a, s);
-  if (a.m <= 4) return linear_rows<4>(a, s);
-  if (a.m <= 8) return linear_rows<8>(a, s);
-  const bool swap = a.m <= 64;
-  const long long P = swap ? a.n : a.m, Q = swap ? a.m : a.n;
-  const long long pt = (P + 127) / 128;
-  int bn = Q <= 16 ? 16 : Q <= 32 ? 32 : Q <= 64 ? 64 : Q <= 128 ? 128 : 256;
-  if (bn == 256 && pt * ((Q + 255) / 256) < sms) bn = 128;
-  if (bn == 128 && pt * ((Q + 127) / 128) < sms) bn = 64;
-  const long long tiles = pt * ((Q + bn - 1) / bn);
-  const int kbs = (a.k + 63) / 64;
-  int splits = 1;
-  if (bn <= 64)
+  if (rows_faster(a)) return linear_rows(a, s);
+  if (a.m <= 64) {  // the channels as an MMA's rows, K split while that gives every SM a tile or two
+    const long long tiles = (a.n + 127) / 128;
+    const int kbs = (a.k + 63) / 64;
+    int splits = 1;
     while (splits < 8 && tiles * splits * 2 <= 2 * sms && kbs >= splits * 8) splits *= 2;
-  switch (bn) {
-    case 16: return linear_al<16, true>(a, splits, status, s);
-    case 32: return linear_al<32, true>(a, splits, status, s);
-    case 64:
-      if (swap) return linear_al<64, true>(a, splits, status, s);
-      if (splits > 1) return linear_al<64, false>(a, splits, status, s);
-      return linear_big<64>(a, sms, status, s);
-    case 128: return linear_big<128>(a, sms, status, s);
-    default:
-      return (a.k & 15) == 0 ? linear_pair_al<true>(a, sms, status, s) : linear_pair_al<false>(a, sms, status, s);
+    if (a.m <= 16) return linear_al<16, true>(a, splits, status, s);
+    if (a.m <= 32) return linear_al<32, true>(a, splits, status, s);
+    return linear_al<64, true>(a, splits, status, s);
+  }
+  switch (pick(a, sms)) {
+    case V_SPLIT2: return linear_al<64, false>(a, 2, status, s);
+    case V_SPLIT4: return linear_al<64, false>(a, 4, status, s);
+    case V_BIG64: return linear_big<64>(a, sms, status, s);
+    case V_BIG128: return linear_big<128>(a, sms, status, s);
+    default: return linear_pair(a, sms, status, s);
   }
 }
 

@@ -130,7 +130,8 @@ def test_linear(m, n, k):
 
 # many tiles: every CTA or pair of them has several, the last ones ragged in all three sizes
 @pytest.mark.parametrize("m,n,k", [(5000, 1000, 208), (5001, 1003, 65), (20000, 264, 64), (9000, 700, 513),
-                                   (40000, 128, 16), (39999, 100, 147), (50000, 64, 160), (50001, 33, 40)])
+                                   (5000, 1000, 2048), (4001, 1003, 1999),
+                                   (3000, 64, 4096), (700, 130, 2600), (40000, 128, 16), (39999, 100, 147), (50000, 64, 160), (50001, 33, 40)])
 def test_linear_many_tiles(m, n, k):
     rng = np.random.default_rng(m + n + k)
     x, sx, w, sw, b = operands(rng, m, n, k)
