@@ -180,11 +180,23 @@ cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long 
 // ---------------------------------------------------------------------------
 namespace {
 
+// 16 bytes that are read once: no line of the L1 for them, so that it keeps the other operand's
+__device__ __forceinline__ uint4 ld_once(const uint4* p) {
+  uint4 v;
+  asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p));
+  return v;
+}
+
 // 16 bytes of a row of k bytes from byte c on, zero past its end; ALIGNED: rows start at multiples
 // of 16 and hold whole vectors.
-template <bool ALIGNED>
+template <bool ALIGNED, bool ONCE = false>
 __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
-  if (ALIGNED) return c < k ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+  if (ALIGNED) {
+    const uint4* p = reinterpret_cast<const uint4*>(row + c);
+    return c < k ? (ONCE ? ld_once(p) : __ldg(p)) : make_uint4(0, 0, 0, 0);
+  }
   if ((k & 7) == 0) {
     const uint2* p = reinterpret_cast<const uint2*>(row + c);
     const uint2 z = make_uint2(0, 0), lo = c < k ? __ldg(p) : z, hi = c + 8 < k ? __ldg(p + 1) : z;
@@ -210,7 +222,7 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
 }  // namespace
 
 template <bool ALIGNED>
-__global__ void __launch_bounds__(256) k_linear_i8_rows(const LinearI8 a) {
+__global__ void __launch_bounds__(256, ALIGNED ? 8 : 5) k_linear_i8_rows(const LinearI8 a) {
   pdl_wait();
   const int lane = (int)threadIdx.x & 31;
   const int j = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), i = (int)blockIdx.y;
@@ -218,16 +230,128 @@ __global__ void __launch_bounds__(256) k_linear_i8_rows(const LinearI8 a) {
   const int8_t* w = a.w + (long long)j * a.k;
   const int8_t* x = a.x + (long long)i * a.k;
   int acc = 0;
-#pragma unroll 2
-  for (int c = lane * 16; c < a.k; c += 512) {
-    const uint4 wv = load16<ALIGNED>(w, c, a.k), xv = load16<ALIGNED>(x, c, a.k);
-    acc = __dp4a((int)wv.x, (int)xv.x, acc);
-    acc = __dp4a((int)wv.y, (int)xv.y, acc);
-    acc = __dp4a((int)wv.z, (int)xv.z, acc);
-    acc = __dp4a((int)wv.w, (int)xv.w, acc);
+#pragma unroll 1
+  for (int c = lane * 16; c < a.k; c += 2048) {
+    uint4 wv[4];  // four loads of the weight in flight
+#pragma unroll
+    for (int u = 0; u < 4; ++u) wv[u] = load16<ALIGNED, true>(w, c + u * 512, a.k);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint4 xv = load16<ALIGNED>(x, c + u * 512, a.k);
+      acc = __dp4a((int)wv[u].x, (int)xv.x, acc);
+      acc = __dp4a((int)wv[u].y, (int)xv.y, acc);
+      acc = __dp4a((int)wv[u].z, (int)xv.z, acc);
+      acc = __dp4a((int)wv[u].w, (int)xv.w, acc);
+    }
   }
   const int s = __reduce_add_sync(0xffffffffu, acc);
   if (lane == 0) a.y[(long long)i * a.n + j] = f2h(fmaf((float)s, a.sx[i] * a.sw[j], a.bias ? h2f(a.bias[j]) : 0.f));
+}
+
+// ---------------------------------------------------------------------------
+// The product for up to 8 NT rows of x on the warps' own matrix instruction
+// (mma.sync m16n8k16, binary16, FP32 sums): 16 RT channels a CTA, K dealt out to its
+// eight warps, 128 bytes a row at a time, and their sums added as integers.  Its rate is
+// a part of tcgen05's, but this product is bound by the weight's bytes, and here
+// they go from memory through the widening into the instruction's registers: no
+// shared memory, no clusters.  (The 8-bit instruction, m16n8k32, takes about 90
+// clocks here and bound the product from 8 rows on.)  A lane holds 16
+// consecutive values of a row where the instruction's layout has pairs eight apart; the
+// same order of K in both operands leaves every sum as it is.
+// ---------------------------------------------------------------------------
+namespace {
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 4 int8 -> 4 binary16: 0x6400 | (x + 128) is 1152 + x
+__device__ __forceinline__ uint2 widen4(uint32_t v) {
+  v ^= 0x80808080u;
+  return make_uint2(hsub2_rn(prmt(v, 0x64646464u, 0x4140u), 0x64806480u),
+                    hsub2_rn(prmt(v, 0x64646464u, 0x4342u), 0x64806480u));
+}
+__device__ __forceinline__ void widen16(const uint4& v, uint32_t (&h)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint2 p = widen4(w[i]);
+    h[2 * i] = p.x;
+    h[2 * i + 1] = p.y;
+  }
+}
+
+}  // namespace
+
+template <int NT, int RT, bool ALIGNED>
+__global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
+  __shared__ int part[8][RT * NT * 4][32];
+  pdl_wait();
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const int j0 = (int)blockIdx.x * (16 * RT), g = lane >> 2, c0 = (lane & 3) * 16;
+  const int8_t* w[2 * RT];
+#pragma unroll
+  for (int r = 0; r < 2 * RT; ++r) {
+    const int j = j0 + r * 8 + g;
+    w[r] = a.w + (long long)(j < a.n ? j : 0) * a.k;
+  }
+  float acc[RT][NT][4];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[r][t][q] = 0.f;
+  constexpr int DEEP = RT > 1 ? 2 : 4;  // chunks of a warp in flight
+#pragma unroll 1
+  for (int c = warp * 128 + c0; c - c0 < a.k; c += DEEP * 512) {  // 128 bytes of a row by a warp, in two loads
+    uint4 u[DEEP][2 * RT];
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+      for (int r = 0; r < 2 * RT; ++r) u[d][r] = load16<ALIGNED, true>(w[r], c + (d >> 1) * 1024 + (d & 1) * 64, a.k);
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) {
+      uint32_t h[2 * RT][8];
+#pragma unroll
+      for (int r = 0; r < 2 * RT; ++r) widen16(u[d][r], h[r]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int i = t * 8 + g;
+        uint32_t b[8];
+        widen16(i < a.m ? load16<ALIGNED>(a.x + (long long)i * a.k, c + (d >> 1) * 1024 + (d & 1) * 64, a.k)
+                         : make_uint4(0, 0, 0, 0),
+                b);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            mma_f16(acc[r][t], h[2 * r][2 * q], h[2 * r + 1][2 * q], h[2 * r][2 * q + 1], h[2 * r + 1][2 * q + 1],
+                    b[2 * q], b[2 * q + 1]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) part[warp][(r * NT + t) * 4 + q][lane] = __float2int_rn(acc[r][t][q]);
+  __syncthreads();
+  // element e: channel e % (16 RT) of row e / (16 RT)
+  for (int e = (int)threadIdx.x; e < RT * NT * 128; e += 256) {
+    const int ch = e % (16 * RT), i = e / (16 * RT);
+    if (i >= a.m || j0 + ch >= a.n) continue;
+    // its accumulator: D[ch & 15][i & 7] of the groups ch >> 4 and i >> 3
+    const int q = ((ch >> 4) * NT + (i >> 3)) * 4 + ((ch >> 3) & 1) * 2 + (i & 1), l = (ch & 7) * 4 + ((i & 7) >> 1);
+    int s = 0;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) s += part[p][q][l];
+    const int col = j0 + ch;
+    a.y[(long long)i * a.n + col] = f2h(fmaf((float)s, a.sx[i] * a.sw[col], a.bias ? h2f(a.bias[col]) : 0.f));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -251,24 +375,19 @@ namespace {
 
 constexpr int kI8Threads = 288;  // eight converting (then storing) warps, one MMA warp
 
+// A stage is 128 values of K, two K-blocks of swizzled tiles: eight lanes load 128 bytes of a row, whole
+// lines.  (Four lanes a row, 64 bytes, took twice the L1's tags.)
 template <int BN>
 struct I8Cfg {
-  static constexpr int STAGE = (128 + BN) * 128;
-  static constexpr int STAGES = 4;
-  static constexpr int DIST = 4;  // K-blocks of raw bytes in registers ahead of the conversion
+  static constexpr int HALF = (128 + BN) * 128;  // one K-block: P's tile, then Q's
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int STAGES = 2;
+  static constexpr int DIST = BN >= 64 ? 2 : 3;  // stages of raw bytes in registers ahead of the conversion
   static constexpr int CTAS = 2;
   static constexpr int SMEM = 1024 + STAGES * STAGE;
-  static constexpr int TMEM = BN < 32 ? 32 : BN;
-  static constexpr int UQ = (BN * 4 + 255) / 256;  // 16-byte units of Q a thread loads per K-block
-  static constexpr int U = 2 + UQ;
+  static constexpr int UP = 4, U = UP + BN / 32;  // 16-byte units a thread loads: of P, of both
 };
 
-// 4 int8 -> 4 binary16
-__device__ __forceinline__ uint2 widen4(uint32_t v) {
-  v ^= 0x80808080u;
-  return make_uint2(hsub2_rn(prmt(v, 0x64646464u, 0x4140u), 0x64806480u),
-                    hsub2_rn(prmt(v, 0x64646464u, 0x4342u), 0x64806480u));
-}
 // 16 int8 as 32 bytes of a tile's row: chunks 2 c and 2 c + 1 of its eight
 __device__ __forceinline__ void put16(uint32_t tile, int row, int c, const uint4& v) {
   const uint2 a = widen4(v.x), b = widen4(v.y), d = widen4(v.z), e = widen4(v.w);
@@ -276,6 +395,43 @@ __device__ __forceinline__ void put16(uint32_t tile, int row, int c, const uint4
   st_shared_v4(at + (uint32_t)(((2 * c) ^ (row & 7)) << 4), make_uint4(a.x, a.y, b.x, b.y));
   st_shared_v4(at + (uint32_t)(((2 * c + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
 }
+// A converting thread's share of the operands, for CTAs with eight converting warps: unit u of a stage is bytes
+// 16 (ct & 7) of row `row` + 32 u of P, or of row `row` + 32 (u - UP) of Q.  The lanes of a row's second 64 bytes,
+// whose K-block's tile lies a multiple of 128 bytes away, take the neighbouring row's instead: its swizzle puts them
+// in the other banks.
+template <int UP, int U, bool ALIGNED>
+struct Feed {
+  const int8_t *const p, *const q;   // the operands, of prows and qrows rows of k
+  const int prows, qrows, k, ct, row;
+  const long long step;
+  const int8_t *pb, *qb;
+  int pl, ql;  // rows from this thread's first to the end
+
+  __device__ __forceinline__ Feed(const int8_t* p_, int prows_, const int8_t* q_, int qrows_, int k_, int ct_)
+      : p(p_), q(q_), prows(prows_), qrows(qrows_), k(k_), ct(ct_), row((ct_ >> 3) ^ ((ct_ >> 2) & 1)),
+        step(32ll * k_) {}
+  // from here on, rows of P from p0 on and of Q from q0 on; none at all if not live
+  __device__ __forceinline__ void place(int p0, int q0, bool live) {
+    pl = live ? prows - (p0 + row) : 0;
+    ql = live ? qrows - (q0 + row) : 0;
+    pb = p + (pl > 0 ? (long long)(p0 + row) * k : 0);
+    qb = q + (ql > 0 ? (long long)(q0 + row) * k : 0);
+  }
+  __device__ __forceinline__ void fetch(int u, int stage, uint4& dst) const {  // (u is a constant where this is expanded)
+    const bool in_p = u < UP;
+    const int i = in_p ? u : u - UP;
+    dst = i * 32 < (in_p ? pl : ql)
+              ? load16<ALIGNED>((in_p ? pb : qb) + i * step, stage * 128 + (ct & 7) * 16, k)
+              : make_uint4(0, 0, 0, 0);
+  }
+  // a unit into the two K-blocks' tiles of a stage, HALF apart: P's 128 rows, then Q's
+  template <int HALF>
+  __device__ __forceinline__ void put(int u, uint8_t* stage, const uint4& v) const {
+    put16(smem_u32(stage) + ((ct >> 2) & 1) * HALF + (u < UP ? 0 : 128 * 128), row + (u < UP ? u : u - UP) * 32,
+          ct & 3, v);
+  }
+};
+
 __device__ __forceinline__ float ld_cluster(uint32_t saddr, uint32_t rank) {
   uint32_t a;
   float v;
@@ -337,7 +493,7 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
     fence_mbar_init();
   }
   if (warp == 8) {
-    tmem_alloc(smem_u32(&tmem_slot), Cfg::TMEM);
+    tmem_alloc(smem_u32(&tmem_slot), BN);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -348,10 +504,8 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
   const int rank = splits > 1 ? (int)cluster_rank() : 0;
   const int tile = (int)blockIdx.x / splits;
   const int p0 = (tile / q_tiles) * 128, q0 = (tile % q_tiles) * BN;
-  const int kbs = (a.k + 63) >> 6, per = (kbs + splits - 1) / splits;
-  const int kb0 = rank * per, kb1 = kb0 + per < kbs ? kb0 + per : kbs;  // (a rank may be left without any)
-  const int nk = kb1 > kb0 ? kb1 - kb0 : 0;
-  const int P = SWAP ? a.n : a.m, Q = SWAP ? a.m : a.n;
+  const int all = (a.k + 127) >> 7, per = (all + splits - 1) / splits;
+  const int s0 = rank * per, ns = max(0, min(per, all - s0));  // stages of this rank (which may have none)
 
   if (warp == 8) {
     if (elect_one()) {
@@ -359,17 +513,21 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
       const uint32_t idesc = idesc_f16(128, BN, false, false, true);
       int stage = 0;
       uint32_t phase = 0;
-      for (int i = 0; i < nk; ++i) {
+      for (int i = 0; i < ns; ++i) {
         if (!mbar_wait(smem_u32(&full[stage]), phase, lim)) {
           atomicCAS(status, 0, -7);  // PF16_ERR_TIMEOUT
           break;
         }
         tc_fence_after();
-        const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE));
-        const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
-          tc_mma_f16(tmem, ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc, i > 0 || kk > 0);
+        for (int h = 0; h < 2; ++h) {
+          if ((s0 + i) * 128 + h * 64 >= a.k) break;
+          const uint32_t s = desc_addr16(smem_u32(smem + stage * Cfg::STAGE + h * Cfg::HALF));
+          const uint64_t ad = desc + s, bd = desc + s + (128 * 128 >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            tc_mma_f16(tmem, ad + (uint64_t)(kk * 2), bd + (uint64_t)(kk * 2), idesc, i > 0 || h > 0 || kk > 0);
+        }
         tc_commit(smem_u32(&empty[stage]));
         if (++stage == Cfg::STAGES) {
           stage = 0;
@@ -381,53 +539,34 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
     }
     __syncwarp();
   } else {
-    // unit u of a K-block: bytes 16 (u & 3) of row u >> 2; P's 512 units first, then Q's
-    const int8_t* base[Cfg::U];
-    bool live[Cfg::U];
-    const int c = tid & 3;
-#pragma unroll
-    for (int i = 0; i < Cfg::U; ++i) {
-      const int r = (tid >> 2) + (i < 2 ? i : i - 2) * 64;
-      const bool in_p = i < 2;
-      const int row = (in_p ? p0 : q0) + r;
-      live[i] = in_p ? row < P : (r < BN && row < Q);
-      const int8_t* from = in_p == SWAP ? a.w : a.x;
-      base[i] = from + (long long)(live[i] ? row : 0) * a.k;
-    }
+    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(SWAP ? a.w : a.x, SWAP ? a.n : a.m, SWAP ? a.x : a.w, SWAP ? a.m : a.n, a.k, tid);
+    feed.place(p0, q0, true);
     uint4 raw[Cfg::DIST][Cfg::U];
-    auto fetch = [&](int i, uint4* dst) {
-      const int at = (kb0 + i) * 64 + c * 16;
+#pragma unroll
+    for (int d = 0; d < Cfg::DIST; ++d)
 #pragma unroll
       for (int u = 0; u < Cfg::U; ++u)
-        dst[u] = live[u] && i < nk ? load16<ALIGNED>(base[u], at, a.k) : make_uint4(0, 0, 0, 0);
-    };
-#pragma unroll
-    for (int d = 0; d < Cfg::DIST; ++d) fetch(d, raw[d]);
+        if (d < ns) feed.fetch(u, s0 + d, raw[d][u]);
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int i = 0; ok && i < nk; i += Cfg::DIST) {
+    for (int i = 0; ok && i < ns; i += Cfg::DIST) {
 #pragma unroll
       for (int d = 0; d < Cfg::DIST; ++d) {
-        if (!ok || i + d >= nk) break;
+        if (!ok || i + d >= ns) break;
         ok = mbar_wait(smem_u32(&empty[stage]), phase ^ 1, lim);
         if (!ok) {
           atomicCAS(status, 0, -7);
           break;
         }
-        const uint32_t sp = smem_u32(smem + stage * Cfg::STAGE), sq = sp + 128 * 128;
 #pragma unroll
         for (int u = 0; u < Cfg::U; ++u) {
-          const int r = (tid >> 2) + (u < 2 ? u : u - 2) * 64;
-          if (u < 2)
-            put16(sp, r, c, raw[d][u]);
-          else if (BN >= 64 || r < BN)
-            put16(sq, r, c, raw[d][u]);
+          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+          if (i + d + Cfg::DIST < ns) feed.fetch(u, s0 + i + d + Cfg::DIST, raw[d][u]);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
-        fetch(i + d + Cfg::DIST, raw[d]);
         if (++stage == Cfg::STAGES) {
           stage = 0;
           phase ^= 1;
@@ -436,30 +575,22 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
     }
     if (!mbar_wait(smem_u32(&done), 0, 2 * lim)) atomicCAS(status, 0, -7);
     tc_fence_after();
-    // the accumulators: rows by the warp's quarter, columns in two halves (one where BN is 16)
+    // the accumulators: rows by the warp's quarter, columns in two halves
     const int row = (warp & 3) * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    constexpr int HALF = BN >= 32 ? BN / 2 : 16;
+    constexpr int HALF = BN / 2;
     const int c0 = (warp >> 2) * HALF;
-    if (splits == 1) {
-      if (c0 < BN) {
+    float* part = reinterpret_cast<float*>(smem);  // [BN][128]: the stages are free
 #pragma unroll 1
-        for (int cc = c0; cc < c0 + HALF; cc += 16) {
-          uint32_t r[16];
-          tmem_ld16(trow + (uint32_t)cc, r);
-          tmem_ld_wait();
-          store_y<SWAP>(a, p0 + row, q0 + cc, reinterpret_cast<const float*>(r), 16);
-        }
-      }
-    } else if (c0 < BN) {
-      float* part = reinterpret_cast<float*>(smem);  // [BN][128]: the stages are free
-#pragma unroll 1
-      for (int cc = c0; cc < c0 + HALF; cc += 16) {
-        uint32_t r[16];
-        tmem_ld16(trow + (uint32_t)cc, r);
-        tmem_ld_wait();
+    for (int cc = c0; cc < c0 + HALF; cc += 16) {
+      uint32_t r[16];
+      tmem_ld16(trow + (uint32_t)cc, r);
+      tmem_ld_wait();
+      if (splits == 1) {
+        store_y<SWAP>(a, p0 + row, q0 + cc, reinterpret_cast<const float*>(r), 16);
+      } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) part[(cc + j) * 128 + row] = nk > 0 ? __uint_as_float(r[j]) : 0.f;
+        for (int j = 0; j < 16; ++j) part[(cc + j) * 128 + row] = ns > 0 ? __uint_as_float(r[j]) : 0.f;
       }
     }
   }
@@ -485,7 +616,7 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
   __syncthreads();
   if (warp == 8 && drained) {
     tc_fence_after();
-    tmem_dealloc(tmem, Cfg::TMEM);
+    tmem_dealloc(tmem, BN);
   }
 }
 
@@ -509,61 +640,6 @@ struct BigCfg {
   static constexpr int DIST = BN >= 128 ? 2 : 3;  // stages of raw bytes in registers
   static constexpr int UP = 4, U = UP + BN / 32;  // 16-byte units of P, of both, that a thread loads per stage
   static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * 4096 + 2 * BN * 8;
-};
-
-// A converting thread's share of the operands: unit u of a stage is bytes 16 (ct & 7) of row `row` + 32 u of
-// P, or of row `row` + 32 (u - UP) of Q.  The lanes of a row's second 64 bytes, whose K-block's tile lies a multiple
-// of 128 bytes away, take the neighbouring row's instead: its swizzle puts them in the other banks.  The raw bytes of DIST stages are in registers.
-// Tile t of this CTA has its rows of P from p0 + ..., given by the caller (`first`, as rows of x and w).
-template <int UP, int U, bool ALIGNED>
-struct Feed {
-  const LinearI8& a;
-  const int ct, row, tiles, ns, step_tile, q_tiles, pm, qm, pofs, qofs;
-  int tile, n, s;  // of the next stage to fetch: the tile, how many tiles before it, the stage in it
-  const int8_t *pb, *qb;
-  int pl, ql;      // rows from this thread's first to the end
-  const long long step;
-
-  // tiles first, first + step_tile, ...; tile t covers rows pm (t / q_tiles) + pofs of x and qm (t % q_tiles) + qofs
-  // of w
-  __device__ __forceinline__ Feed(const LinearI8& a_, int ct_, int first, int step_tile_, int tiles_, int ns_,
-                                  int q_tiles_, int pm_, int qm_, int pofs_, int qofs_)
-      : a(a_), ct(ct_), row((ct_ >> 3) ^ ((ct_ >> 2) & 1)), tiles(tiles_), ns(ns_), step_tile(step_tile_), q_tiles(q_tiles_), pm(pm_), qm(qm_),
-        pofs(pofs_), qofs(qofs_), tile(first), n(0), s(0), step(32ll * a_.k) {
-    place();
-  }
-  __device__ __forceinline__ void place() {
-    const int pr = (tile / q_tiles) * pm + pofs + row, qr = (tile % q_tiles) * qm + qofs + row;
-    pl = n < tiles ? a.m - pr : 0;
-    ql = n < tiles ? a.n - qr : 0;
-    pb = a.x + (pl > 0 ? (long long)pr * a.k : 0);
-    qb = a.w + (ql > 0 ? (long long)qr * a.k : 0);
-  }
-  __device__ __forceinline__ void fetch(int u, uint4& dst) const {  // (u is a constant where this is expanded)
-    const bool p = u < UP;
-    const int i = p ? u : u - UP;
-    dst = i * 32 < (p ? pl : ql) ? load16<ALIGNED>((p ? pb : qb) + i * step, s * 128 + (ct & 7) * 16, a.k)
-                                 : make_uint4(0, 0, 0, 0);
-  }
-  __device__ __forceinline__ void next() {
-    if (++s == ns) {
-      s = 0;
-      ++n;
-      tile += step_tile;
-      place();
-    }
-  }
-  // converts a stage into its two K-blocks' tiles at `half` (P's, then Q's) and fetches a later one in its place
-  __device__ __forceinline__ void convert(uint4 (&raw)[U], uint32_t half) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      put16(half + (u < UP ? 0 : 128 * 128), row + (u < UP ? u : u - UP) * 32, ct & 3, raw[u]);
-      fetch(u, raw[u]);
-    }
-    next();
-    fence_proxy_async_smem();
-    __syncwarp();
-  }
 };
 
 // What a storing thread reads of a tile before it stores it: the scales of its four rows (r0 + 8 i + (lane >> 2)) and
@@ -766,13 +842,26 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     }
   } else {
     const int ct = tid - 160;
-    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a, ct, (int)blockIdx.x, (int)gridDim.x, mine, ns, q_tiles, 128, BN, 0, 0);
+    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a.x, a.m, a.w, a.n, a.k, ct);
+    int fn = 0, fs = 0;  // of the next stage to fetch: the tile, the stage in it
+    auto place = [&]() {
+      const int tile = (int)blockIdx.x + fn * (int)gridDim.x;
+      feed.place((tile / q_tiles) * 128, (tile % q_tiles) * BN, fn < mine);
+    };
+    auto next = [&]() {
+      if (++fs == ns) {
+        fs = 0;
+        ++fn;
+        place();
+      }
+    };
+    place();
     uint4 raw[Cfg::DIST][Cfg::U];
 #pragma unroll
     for (int d = 0; d < Cfg::DIST; ++d) {
 #pragma unroll
-      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, raw[d][u]);
-      feed.next();
+      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, fs, raw[d][u]);
+      next();
     }
     int stage = 0;
     uint32_t phase = 0;
@@ -787,7 +876,14 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           atomicCAS(status, 0, -7);
           break;
         }
-        feed.convert(raw[d], smem_u32(smem + stage * Cfg::STAGE + ((ct >> 2) & 1) * Cfg::HALF));
+#pragma unroll
+        for (int u = 0; u < Cfg::U; ++u) {
+          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+          feed.fetch(u, fs, raw[d][u]);
+        }
+        next();
+        fence_proxy_async_smem();
+        __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
         if (++stage == Cfg::STAGES) {
           stage = 0;
@@ -940,13 +1036,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
   } else if (warp <= 12) {
     const int ct = tid - 160;
-    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a, ct, pair, pairs, mine, ns, q_tiles, 256, 256, rank * 128, rank * 128);
+    Feed<Cfg::UP, Cfg::U, ALIGNED> feed(a.x, a.m, a.w, a.n, a.k, ct);
+    int fn = 0, fs = 0;  // of the next stage to fetch: the tile, the stage in it
+    auto place = [&]() {
+      const int tile = pair + fn * pairs;
+      feed.place((tile / q_tiles) * 256 + rank * 128, (tile % q_tiles) * 256 + rank * 128, fn < mine);
+    };
+    auto next = [&]() {
+      if (++fs == ns) {
+        fs = 0;
+        ++fn;
+        place();
+      }
+    };
+    place();
     uint4 raw[Cfg::DIST][Cfg::U];
 #pragma unroll
     for (int d = 0; d < Cfg::DIST; ++d) {
 #pragma unroll
-      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, raw[d][u]);
-      feed.next();
+      for (int u = 0; u < Cfg::U; ++u) feed.fetch(u, fs, raw[d][u]);
+      next();
     }
     int stage = 0;
     uint32_t phase = 0;
@@ -961,7 +1070,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           atomicCAS(status, 0, -7);
           break;
         }
-        feed.convert(raw[d], smem_u32(smem + stage * Cfg::STAGE + ((ct >> 2) & 1) * Cfg::HALF));
+#pragma unroll
+        for (int u = 0; u < Cfg::U; ++u) {
+          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+          feed.fetch(u, fs, raw[d][u]);
+        }
+        next();
+        fence_proxy_async_smem();
+        __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
         if (++stage == Cfg::STAGES) {
           stage = 0;
@@ -1071,14 +1187,30 @@ cudaError_t linear_rows(const LinearI8& a, cudaStream_t s) {
   return e == cudaSuccess ? counted_launches(1) : e;
 }
 
+template <int NT, int RT>
+cudaError_t linear_few(const LinearI8& a, cudaStream_t s) {
+  const dim3 grid((unsigned)((a.n + 16 * RT - 1) / (16 * RT)));
+  const cudaError_t e = (a.k & 15) == 0 ? launch_pdl(k_linear_i8_few<NT, RT, true>, grid, dim3(256), 0, s, a)
+                                        : launch_pdl(k_linear_i8_few<NT, RT, false>, grid, dim3(256), 0, s, a);
+  return e == cudaSuccess ? counted_launches(1) : e;
+}
+
 // The variants' times in microseconds, as measured and interpolated, from the sizes alone.
 //
-// One warp an element against the tensor cores with 128 channels in an MMA's rows (m n k: us, us):
-//   8 1000 2048: 2.8, 6.2    6 2048 2048: 3.9, 6.7    12 4096 1024: 5.8, 5.9    2 8192 8192: 17.4, 20.5
-//   4 8192 8192: 26.7, 20.7  8 8192 8192: 42.8, 21.0
+// A warp an element: from HBM once, from the L2 for further rows (b = n k bytes):
+//   m n k          warps  mma.sync        m n k          warps  mma.sync
+//   2 1008 2048     2.1     2.6           2 8192 8192    15.9    15.3
+//   8 1008 2048     2.8     2.6           8 8192 8192    39.0    15.4
 bool rows_faster(const LinearI8& a) {
-  const double bytes = (double)a.n * a.k;
-  return a.m <= 32 && 1.8 + a.m * bytes / 12.5e6 < 5.5 + bytes / 4.4e6;
+  const double b = (double)a.n * a.k;
+  return a.m == 1 || (a.m <= 8 && 1.8 + a.m * b / 10e6 < 2.2 + b / 5e6);
+}
+// mma.sync for up to 32 rows against tcgen05 with the channels as its rows and K split over a cluster:
+//   16 1008 2048    2.8, 6.2    16 8192 8192   18.5, 23.6    32 1008 2048  4.1, 6.4
+//   32 4096 1024    3.9, 5.9    32 8192 8192   28.2, 21.5
+bool few_faster(const LinearI8& a) {
+  const double b = (double)a.n * a.k;
+  return a.m <= 16 || (a.m <= 32 && 3.2 + b / 2.7e6 < 5.5 + b / 4.2e6);
 }
 
 enum Variant { V_SPLIT2, V_SPLIT4, V_BIG64, V_BIG128, V_PAIR };
@@ -1115,14 +1247,19 @@ Variant pick(const LinearI8& a, int sms) {
 
 cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s) {
   if (rows_faster(a)) return linear_rows(a, s);
+  if (few_faster(a)) {
+    // 32 channels a CTA halve the reads of x, 16 fill the SMs: 16 8192 8192 18.5, 22.1; 16 1008 2048 3.6, 2.8
+    const bool wide = a.n >= 16 * sms;
+    if (a.m <= 8) return linear_few<1, 1>(a, s);
+    if (a.m <= 16) return wide ? linear_few<2, 2>(a, s) : linear_few<2, 1>(a, s);
+    return wide ? linear_few<4, 2>(a, s) : linear_few<4, 1>(a, s);
+  }
   if (a.m <= 64) {  // the channels as an MMA's rows, K split while that gives every SM a tile or two
     const long long tiles = (a.n + 127) / 128;
     const int kbs = (a.k + 63) / 64;
     int splits = 1;
     while (splits < 8 && tiles * splits * 2 <= 2 * sms && kbs >= splits * 8) splits *= 2;
-    if (a.m <= 16) return linear_al<16, true>(a, splits, status, s);
-    if (a.m <= 32) return linear_al<32, true>(a, splits, status, s);
-    return linear_al<64, true>(a, splits, status, s);
+    return a.m <= 32 ? linear_al<32, true>(a, splits, status, s) : linear_al<64, true>(a, splits, status, s);
   }
   switch (pick(a, sms)) {
     case V_SPLIT2: return linear_al<64, false>(a, 2, status, s);

@@ -116,7 +116,8 @@ def check_linear(x, sx, w, sw, bias, y):
 LINEAR = [(1, 1, 1), (1, 8, 16), (1, 1000, 2048), (2, 100, 64), (3, 5, 33), (4, 129, 128), (5, 64, 100), (7, 300, 15),
           (8, 1000, 512), (9, 257, 160), (16, 512, 1040), (17, 65, 65), (31, 1001, 77), (33, 128, 2048), (64, 64, 64),
           (65, 200, 192), (100, 1000, 2048), (127, 127, 127), (128, 256, 512), (129, 255, 144), (256, 1000, 2048),
-          (300, 520, 1088), (1000, 64, 256), (640, 384, 48), (513, 1024, 320), (2, 8192, 96), (40, 3000, 4608)]
+          (300, 520, 1088), (1000, 64, 256), (640, 384, 48), (513, 1024, 320), (2, 8192, 96), (40, 3000, 4608), (12, 2500, 200), (15, 2437, 77), (20, 2500, 136), (29, 3001, 250),
+          (32, 8192, 2304), (23, 8190, 2305), (10, 40, 5000)]
 
 
 @pytest.mark.parametrize("m,n,k", LINEAR)
@@ -138,7 +139,8 @@ def test_linear_many_tiles(m, n, k):
     check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
 
 
-@pytest.mark.parametrize("m,n,k", [(5000, 1000, 1024), (40000, 128, 1024), (1, 64, 1024), (6, 130, 1024), (130, 70, 1024), (20, 260, 1024), (300, 300, 1024)])
+@pytest.mark.parametrize("m,n,k", [(5000, 1000, 1024), (40000, 128, 1024), (1, 64, 1024), (6, 130, 1024), (130, 70, 1024), (20, 260, 1024), (300, 300, 1024), (16, 2600, 1024), (9, 33, 1024),
+                                   (30, 2600, 1024)])
 def test_linear_sums_are_exact(m, n, k):
     """Scales of one: sums up to 1024 * 128^2 = 2^24 come out as binary16 rounds the exact integers
     (scaled so that none overflows)."""
@@ -150,7 +152,8 @@ def test_linear_sums_are_exact(m, n, k):
     assert np.array_equal(linear(x, sx, w, sw, None), want.astype(np.float16))
 
 
-@pytest.mark.parametrize("m,n,k", [(3, 40, 4608), (50, 300, 5000), (200, 200, 8192), (1, 9, 65536), (70, 9, 65536)])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 4608), (50, 300, 5000), (200, 200, 8192), (1, 9, 65536), (70, 9, 65536), (7, 600, 9000),
+                                   (16, 2500, 6001), (31, 40, 65536)])
 def test_linear_long_sums(m, n, k):
     rng = np.random.default_rng(k)
     x, sx, w, sw, b = operands(rng, m, n, k, extreme=True)
