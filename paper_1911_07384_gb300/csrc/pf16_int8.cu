@@ -193,10 +193,9 @@ __device__ __forceinline__ uint4 ld_once(const uint4* p) {
 // of 16 and hold whole vectors.
 template <bool ALIGNED, bool ONCE = false>
 __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
-  if (ALIGNED) {
-    const uint4* p = reinterpret_cast<const uint4*>(row + c);
-    return c < k ? (ONCE ? ld_once(p) : __ldg(p)) : make_uint4(0, 0, 0, 0);
-  }
+  // (the pointer inside the guard: named before it, the load became a branch, and large products 10% slower)
+  if (ALIGNED && ONCE) return c < k ? ld_once(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+  if (ALIGNED) return c < k ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
   if ((k & 7) == 0) {
     const uint2* p = reinterpret_cast<const uint2*>(row + c);
     const uint2 z = make_uint2(0, 0), lo = c < k ? __ldg(p) : z, hi = c + 8 < k ? __ldg(p + 1) : z;

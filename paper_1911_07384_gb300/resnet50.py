@@ -29,6 +29,8 @@ WD = 0x068E       # 1e-4 (1.00016594e-4)
 EPS = 0x00A8      # 1e-5 (subnormal, 1.00135803e-5)
 S_BLOCK = 0x3400  # 0.25: BatchNorms inside residual blocks
 S_STEM = 0x3C00   # 1.0: the stem BatchNorm
+# the orthogonalised update (optimizer="muon"): floats, its arithmetic between the stored tensors is FP32
+MUON_LR, MUON_MOMENTUM, MUON_WD = 0.02, 0.95, 1e-4
 
 STAGES = [(64, 3, 1), (128, 4, 2), (256, 6, 2), (512, 3, 2)]  # width, blocks, stride
 
@@ -355,7 +357,7 @@ class ResNet50:
     """Buffers and call sequence of one pure-FP16 ResNet-50 training step."""
 
     def __init__(self, batch=256, image=224, classes=1000, device="cuda", seed_cfg=4, hook=None, bn_swap=False,
-                 wgrad_branch=False, exchange=None, bn_in_operand=False, stem_fused=True):
+                 wgrad_branch=False, exchange=None, bn_in_operand=False, stem_fused=True, optimizer="sgd"):
         """wgrad_branch: issue the weight gradients on a second stream that joins
         before the update (in a captured step graph: a parallel branch), so that
         they fill the gaps of the data-gradient chain; off, every call runs on the
@@ -372,7 +374,13 @@ class ResNet50:
         fill the SM's issue slots).
         stem_fused: the stem's BatchNorm, ReLU and max pooling forward run as
         one call (pf16_bn_relu_maxpool_fwd: bit-identical results, the
-        BatchNorm's output never stored)."""
+        BatchNorm's output never stored).
+        optimizer: "sgd", the paper's recipe, or "muon": the convolutions' filters, as [k][r*s*c]
+        matrices, take orthogonalised updates (pf16_muon_update, all of them in one call) and the
+        classifier and the BatchNorms the same SGD as before."""
+        if optimizer not in ("sgd", "muon"):
+            raise ValueError(f"optimizer {optimizer!r}: \"sgd\" or \"muon\"")
+        self.optimizer = optimizer
         self.N, self.image, self.classes, self.device = batch, image, classes, device
         self.stem_fused = stem_fused
         self.hook = hook  # optional callable(kind, layer, fn, *args) used for instrumentation
@@ -438,6 +446,11 @@ class ResNet50:
             ws = max(ws, pf16.bn_workspace_size(b.desc))
         ws = max(ws, pf16.softmax_xent_workspace_size(N, self.classes))
         self.ws = torch.empty(ws, dtype=torch.uint8, device=dev)
+        if self.optimizer == "muon":
+            self.muon = pf16.muon_list(
+                (c.w, self.wd.view("v", c.off, c.numel), c.gw, c.desc.k, c.numel // c.desc.k,
+                 max(1.0, c.desc.k * c.desc.k / c.numel) ** 0.5) for c in self.convs if c is not self.fc)
+            self.ws_muon = torch.empty(pf16.muon_workspace_size(self.muon), dtype=torch.uint8, device=dev)
         # the weight gradients' own scratch when they run on the side branch
         wsw = max(pf16.conv_workspace_size(c.desc, pf16.PF16_PASS_WGRAD) for c in self.convs)
         self.ws_w = torch.empty(max(wsw, 256), dtype=torch.uint8, device=dev) if self.side is not None else None
@@ -508,13 +521,38 @@ class ResNet50:
         if self.exchange is not None:  # the ranks' gradients averaged, in a fixed FP16 order
             self.call("exchange", None, self.exchange, self.wd.g)
             self.call("exchange", None, self.exchange, self.nowd.g)
-        self.call("sgd", None, pf16.sgd_update, self.wd.w, self.wd.v, self.wd.g, LR, MOMENTUM, WD)
+        rest = 0  # of the decayed arena: all of it, or the classifier (its weight and bias are the arena's end)
+        if self.optimizer == "muon":
+            self.call("muon", None, pf16.muon_update, self.muon, MUON_LR, MUON_MOMENTUM, MUON_WD, self.ws_muon)
+            rest = self.fc.off
+        self.call("sgd", None, pf16.sgd_update, self.wd.w[rest:], self.wd.v[rest:], self.wd.g[rest:], LR, MOMENTUM, WD)
         self.call("sgd", None, pf16.sgd_update, self.nowd.w, self.nowd.v, self.nowd.g, LR, MOMENTUM, 0)
 
     def step(self):
         self.forward()
         self.backward()
         self.update()
+
+    # ------------------------------------------------------------- 8-bit classifier
+    def quantize_classifier(self):
+        """The classifier's weight as 8-bit rows with a scale each (again after an update)."""
+        k, c = self.classes, self.cl
+        if not hasattr(self, "fc8"):
+            new = lambda n, dtype: torch.empty(n, dtype=dtype, device=self.device)
+            self.fc8, self.fc8_scale = new(k * c, torch.int8), new(k, torch.float32)
+            self.f8, self.f8_scale = new(self.N * c, torch.int8), new(self.N, torch.float32)
+            self.logits8 = new((self.N, k), torch.float16)
+        self.call("quantize", self.fc, pf16.quantize_i8, self.fc.w, self.fc8, self.fc8_scale, k, c)
+
+    def classify_i8(self):
+        """Logits, bias included, of the last forward's features through the quantised classifier: each
+        image's features as one 8-bit row.  float16 [batch][classes], overwritten by the next call."""
+        if not hasattr(self, "fc8"):
+            raise RuntimeError("classify_i8 before quantize_classifier")
+        self.call("quantize", None, pf16.quantize_i8, self.f, self.f8, self.f8_scale, self.N, self.cl)
+        self.call("linear_i8", self.fc, pf16.linear_i8, self.f8, self.f8_scale, self.fc8, self.fc8_scale, self.bias,
+                  self.logits8, self.N, self.classes, self.cl)
+        return self.logits8
 
     # ------------------------------------------------------------- accounting
     def conv_flops(self):

@@ -1,0 +1,95 @@
+"""The orthogonalised update and the 8-bit classifier as the network's step and its answers use them."""
+import numpy as np
+import pytest
+
+import matrix_oracle as mo
+from gpu_util import dev, f64, host
+from paper_1911_07384_gb300 import pf16
+from paper_1911_07384_gb300 import resnet50 as rn
+from paper_1911_07384_gb300 import synthetic as syn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def net():
+    n = rn.ResNet50(batch=2, image=64, classes=40, seed_cfg=4, optimizer="muon")
+    n.set_batch(syn.images_f16(syn.seed_for(4, "x"), 2, 64, 64, 3), syn.labels(syn.seed_for(4, "labels"), 2) % 40)
+    return n
+
+
+def test_step_with_orthogonalised_updates(net, orc):
+    assert len(net.muon) == 53
+    for _ in range(2):  # the second step has momentum
+        net.forward()
+        net.backward()
+        assert pf16.sync_status() == 0
+        before = {(a.name, s): host(getattr(a, s)).copy() for a in (net.wd, net.nowd) for s in "wvg"}
+        net.update()
+        assert pf16.sync_status() == 0
+        after = {(a.name, s): host(getattr(a, s)).copy() for a in (net.wd, net.nowd) for s in "wv"}
+        for c in net.convs[:-1]:
+            rows, cols = c.desc.k, c.numel // c.desc.k
+            w, v, g = (f64(before["decayed", s][c.off:c.off + c.numel]).reshape(rows, cols) for s in "wvg")
+            assert np.isfinite(g).all()
+            scale = max(1.0, rows / cols) ** 0.5
+            w64, v64, u = mo.muon(w, v, g, rn.MUON_LR, rn.MUON_MOMENTUM, rn.MUON_WD, scale, True)
+            nv = f64(after["decayed", "v"][c.off:c.off + c.numel]).reshape(rows, cols)
+            assert np.all(np.abs(nv - v64) <= (mo.U16 + 2.0 ** -23) * np.abs(v64) + mo.TINY16)
+            nw = f64(after["decayed", "w"][c.off:c.off + c.numel]).reshape(rows, cols)
+            tol = rn.MUON_LR * scale * mo.orthogonal_tolerance(u) + (mo.U16 + 2.0 ** -21) * np.linalg.norm(w64)
+            assert np.linalg.norm(nw - w64) <= tol + mo.TINY16 * np.sqrt(w.size), (rows, cols)
+        # the classifier and the BatchNorms: SGD, bit for bit
+        for name, start, wd in (("decayed", net.fc.off, rn.WD), ("no-decay", 0, 0)):
+            ew, ev = orc.sgd_update(*(before[name, s][start:] for s in "wvg"), rn.LR, rn.MOMENTUM, wd)
+            assert np.array_equal(after[name, "w"][start:], ew) and np.array_equal(after[name, "v"][start:], ev)
+
+
+def test_step_captured(net):
+    """Steps of a captured graph are the eager steps' bits."""
+    import torch
+
+    start = {(a, s): getattr(a, s).clone() for a in (net.wd, net.nowd) for s in "wv"}
+
+    def rewind():
+        for (a, s), t in start.items():
+            getattr(a, s).copy_(t)
+
+    for _ in range(2):
+        net.step()
+    assert pf16.sync_status() == 0
+    eager = [host(a.w).copy() for a in (net.wd, net.nowd)]
+    rewind()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        net.step()
+    torch.cuda.synchronize()
+    rewind()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert pf16.sync_status() == 0
+    for a, e in zip((net.wd, net.nowd), eager):
+        assert np.array_equal(host(a.w), e)
+    rewind()
+
+
+def test_classifier_in_eight_bits(net):
+    net.forward()
+    net.quantize_classifier()
+    got = net.classify_i8()
+    assert pf16.sync_status() == 0
+    f, w = (host(t).view(np.float16) for t in (net.f, net.fc.w))
+    fq, fs = mo.quantize(f.reshape(2, -1))
+    wq, ws = mo.quantize(w.reshape(40, -1))
+    want, slack = mo.linear(fq, fs.astype(np.float32), wq, ws.astype(np.float32), host(net.bias).view(np.float16))
+    err = np.abs(got.cpu().numpy().astype(np.float64) - want)
+    assert np.all(err <= slack + mo.U16 * (np.abs(want) + slack) + mo.TINY16)
+
+
+def test_refusals():
+    with pytest.raises(ValueError, match="optimizer"):
+        rn.ResNet50(batch=2, image=64, optimizer="adam")
+    with pytest.raises(RuntimeError, match="quantize_classifier"):
+        rn.ResNet50(batch=2, image=64).classify_i8()
