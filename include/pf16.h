@@ -408,7 +408,8 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  * between 0.68 and 1.21 for all but the smallest.  X is held in FP32; the
  * products take binary16 copies (scaled by powers of two) and accumulate in
  * FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
- * norm is not finite gives NaNs throughout.  Same inputs, same bits.
+ * norm is not finite gives NaNs throughout.  Same inputs, same bits,
+ * whatever else the call holds.
  *
  * All matrices of one call run together, in three launches.  1 <= rows, cols <=
  * 65536, rows * cols <= 2^30, at most PF16_ORTHO_MAX_MATRICES matrices

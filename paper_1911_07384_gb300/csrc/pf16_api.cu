@@ -1679,7 +1679,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
   const size_t words = 4 + (size_t)count;
-  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0, blocks = 0;
+  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0;
   for (int i = 0; i < count; ++i) {
     const OrthoEntry& s = e[order[i]];
     OrthoMat& m = p->mat[i];
@@ -1695,16 +1695,18 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     m.part0 = (int)parts;
     m.parts = ortho_parts((long long)s.rows * s.cols);
     parts += m.parts;
-    blocks += (long long)ortho_sym(ortho_tiles(m.mb)) * m.nb;
+    m.precise = m.mb <= kOrthoPrecise;
   }
-  // X X^T's sums split so that an item's share is near a pair's share of them all, but no less
-  // than 12 blocks (about 3 us; the parts' store, their phase and its wait take about 8).
-  const long long share = std::max(12ll, blocks / kOrthoPairs);
   for (int i = 0; i < count; ++i) {
     OrthoMat& m = p->mat[i];
-    m.splits = (int)std::min<long long>(8, std::max<long long>(1, m.nb / share));
-    m.kper = cdiv(m.nb, m.splits);
-    m.splits = cdiv(m.nb, m.kper);
+    const int terms = m.precise ? 3 * m.nb : m.nb;
+    // X X^T's sum split so that the matrix would keep every pair of SMs busy, but into no less than 16 blocks
+    // (about 4 us; the parts' store, their phase and its wait take about 8).  By its own size alone: the split
+    // decides the order of the sum, which the other matrices of a call must not.
+    const long long share = std::max(16ll, (long long)ortho_sym(ortho_tiles(m.mb)) * terms / kOrthoPairs);
+    m.splits = (int)std::min<long long>(8, std::max<long long>(1, terms / share));
+    m.kper = cdiv(terms, m.splits);
+    m.splits = cdiv(terms, m.kper);
     const int mt = ortho_tiles(m.mb), nt = ortho_tiles(m.nb), tri = ortho_sym(mt);
     p->pre_pack[i] = (int)pack;
     p->pre_gram[i] = (int)gram;
@@ -1730,7 +1732,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   at += round_up((size_t)parts * 4, 256);
   for (int i = 0; i < count; ++i) {
     p->mat[i].ws = base + at;
-    at += ortho_layout(p->mat[i].mb, p->mat[i].nb, p->mat[i].splits).bytes;
+    at += ortho_layout(p->mat[i].mb, p->mat[i].nb, p->mat[i].splits, p->mat[i].precise).bytes;
   }
   return at;
 }

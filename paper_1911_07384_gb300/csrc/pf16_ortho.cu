@@ -92,6 +92,14 @@ __device__ __forceinline__ float2 h22f(uint32_t v) {
   return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
 
+// what rounding to the pair h leaves of x, y
+__device__ __forceinline__ uint32_t low2(float x, float y, uint32_t h) {
+  const float2 f = h22f(h);
+  return f2h2(x - f.x, y - f.y);
+}
+// blocks in the sum over n of them: with two copies of the operands, three times as many
+__device__ __forceinline__ int ortho_sum(int n, int precise) { return precise ? 3 * n : n; }
+
 // the largest i with pre[i] <= t, pre[0] = 0 and t < pre[n]
 __device__ __forceinline__ int find_mat(const int* pre, int n, int t) {
   int lo = 0, hi = n;
@@ -137,7 +145,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     it.split = local % M.splits;
     sym_tile(local / M.splits, it.I, it.J);
     it.k0 = it.split * M.kper;
-    it.k1 = min(it.k0 + M.kper, M.nb);
+    it.k1 = min(it.k0 + M.kper, ortho_sum(M.nb, M.precise));
   } else if (t < (uint32_t)(tg + ta)) {
     t -= (uint32_t)tg;
     it.kind = kSum;
@@ -151,7 +159,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     it.kind = kSym;
     it.mat = find_mat(p.pre_sym, n, (int)t);
     sym_tile((int)t - p.pre_sym[it.mat], it.I, it.J);
-    it.k1 = p.mat[it.mat].mb;
+    it.k1 = ortho_sum(p.mat[it.mat].mb, p.mat[it.mat].precise);
   } else {
     t -= (uint32_t)(tg + ta + ts);
     it.kind = kFull;
@@ -160,7 +168,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     const int mt = ortho_tiles(p.mat[it.mat].mb);
     it.I = local % mt;  // column by column: neighbours share X's blocks
     it.J = local / mt;
-    it.k1 = p.mat[it.mat].mb;
+    it.k1 = ortho_sum(p.mat[it.mat].mb, p.mat[it.mat].precise);
   }
   const OrthoMat& M = p.mat[it.mat];
   const int mt = ortho_tiles(M.mb), nt = ortho_tiles(M.nb);
@@ -322,7 +330,7 @@ __global__ void __launch_bounds__(256) k_ortho_pack(const __grid_constant__ Orth
     tile[M.tall ? cc * kPackPitch + rr : rr * kPackPitch + cc] = x;
   }
   __syncthreads();
-  const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
+  const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits, M.precise);
   uint8_t* x32 = M.ws + L.x32 + ((size_t)bi * M.nb + bj) * (2 * kOrthoBlk);
   uint8_t* x16 = M.ws + L.x16 + ortho_block(bi, bj, (M.nb + 1) & ~1) * kOrthoBlk;
 #pragma unroll
@@ -340,6 +348,14 @@ __global__ void __launch_bounds__(256) k_ortho_pack(const __grid_constant__ Orth
     v.y = f2h2(s[2] * kSx, s[3] * kSx);
     v.z = f2h2(s[4] * kSx, s[5] * kSx);
     v.w = f2h2(s[6] * kSx, s[7] * kSx);
+    if (M.precise) {
+      const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+      uint32_t lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lo[j] = low2(s[2 * j] * kSx, s[2 * j + 1] * kSx, h[j]);
+      *reinterpret_cast<uint4*>(x16 + L.lo + row * 128 + ((ch ^ (row & 7)) << 4)) =
+          make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
     *reinterpret_cast<uint4*>(x16 + row * 128 + ((ch ^ (row & 7)) << 4)) = v;
   }
 }
@@ -416,13 +432,26 @@ __device__ __forceinline__ bool is_mn(int kind, bool right, int tile, int kb) {
   if (kind == kFull && right) return true;
   return (kb >> 2) > tile;
 }
-// The end of the run of blocks from kb on in which both operands keep their form.
-__device__ __forceinline__ int run_end(const Item& it, int kb) {
-  int e = it.k1;
-  if (it.kind == kGram) return e;
-  if ((kb >> 2) <= it.I) e = min(e, it.I * 4 + 4);
-  if (it.kind == kSym && (kb >> 2) <= it.J) e = min(e, it.J * 4 + 4);
-  return e;
+// The sum's blocks [at, end) in which both operands keep their form: block kb of the operands on, `part` being 0 for
+// the high copies' products, 1 and 2 for those with the right and the left one's low copy.
+struct Run {
+  int kb, part, end;
+  bool a_mn, b_mn;
+  __device__ __forceinline__ Run(const Item& it, const OrthoMat& M, int at) {
+    const int n = it.kind == kGram ? M.nb : M.mb;
+    part = at / n;
+    kb = at - part * n;
+    int e = n;
+    if (it.kind != kGram && (kb >> 2) <= it.I) e = min(e, it.I * 4 + 4);
+    if (it.kind == kSym && (kb >> 2) <= it.J) e = min(e, it.J * 4 + 4);
+    end = min(it.k1, part * n + e);
+    a_mn = is_mn(it.kind, false, it.I, kb);
+    b_mn = is_mn(it.kind, true, it.J, kb);
+  }
+};
+// Whether one operand tile serves as both: on the diagonal, of single copies.
+__device__ __forceinline__ bool same_operand(const Item& it, const OrthoMat& M) {
+  return it.kind != kFull && it.I == it.J && !M.precise;
 }
 
 // One 8 KB block of the workspace, which `map` describes as rows of 128 bytes, signalling the leading
@@ -468,6 +497,7 @@ struct TileOut {
   uint32_t stage_w;
   int chunks, rr, lane, row, bj0;
   bool full_kind, final_step;
+  size_t lo;            // to the low copies, or 0
 
   // what chunk c adds to its product, raw: X, or S in binary16
   __device__ __forceinline__ void load(int c, uint4* v) const {
@@ -516,6 +546,21 @@ struct TileOut {
           x[i + 1] = __float_as_uint(fmaf(__uint_as_float(x[i + 1]), mul, f.y * (kB * kSb / kSa)));
         }
       }
+      if (lo) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 o = __ldcg(reinterpret_cast<const uint4*>(a16 + lo + (c >> 1) * (2 * kOrthoBlk) +
+                                                                ((((c & 1) * 4 + j) ^ (rr & 7)) << 4)));
+          const uint32_t h[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float2 f = h22f(h[q]);
+            const int i = 8 * j + 2 * q;
+            x[i] = __float_as_uint(fmaf(f.x, kB * kSb / kSa, __uint_as_float(x[i])));
+            x[i + 1] = __float_as_uint(fmaf(f.y, kB * kSb / kSa, __uint_as_float(x[i + 1])));
+          }
+        }
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * mul);
@@ -525,6 +570,19 @@ struct TileOut {
       __syncwarp();
     }
     const float* f = reinterpret_cast<const float*>(x);
+    if (lo) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t l[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          l[q] = low2(f[8 * h + 2 * q], f[8 * h + 2 * q + 1], f2h2(f[8 * h + 2 * q], f[8 * h + 2 * q + 1]));
+        __stcg(reinterpret_cast<uint4*>(out + lo + (c >> 1) * (2 * kOrthoBlk) + lane * 128 +
+                                        ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
+               make_uint4(l[0], l[1], l[2], l[3]));
+      }
+      fence_proxy_async_all();  // the operand copies read them
+    }
 #pragma unroll
     for (int h = 0; h < 4; ++h)
       st_shared_v4(stage_w + (uint32_t)(lane * 128 + ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
@@ -643,23 +701,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (it.kind == kSum) continue;
         fence_proxy_async_all();  // the blocks' writers used both proxies
         const OrthoMat& M = p.mat[it.mat];
-        const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
+        const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits, M.precise);
         const int base = (int)((M.ws - p.ws) >> 7);
-        const int X = base + (int)((L.x16 + (it.step & 1) * (L.x32 / 2)) >> 7);
+        const int X = base + (int)((L.x16 + (it.step & 1) * (L.a16 / 2)) >> 7);
         const int S = base + (int)((it.kind == kFull ? L.b16 : L.a16) >> 7);  // the symmetric operand
         const int me = (M.mb + 1) & ~1, ne = (M.nb + 1) & ~1;
         const int ra = it.I * 4 + (int)rank * 2, rb = it.J * 4 + (int)rank * 2;  // first row of blocks
-        const bool same = it.kind != kFull && it.I == it.J;                      // one operand serves as both
+        const bool same = same_operand(it, M);
         const int rows_b = it.kind == kFull ? M.nb : M.mb;
         const bool la = ra < M.mb, lb = !same && rb < rows_b;
         // both CTAs' bytes (the first rows of a tile, the leading CTA's, are never past the edge)
         const uint32_t bytes = 2 * kOrthoBlk * (uint32_t)(1 + (it.I * 4 + 2 < M.mb ? 1 : 0) +
                                                           (same ? 0 : 1 + (it.J * 4 + 2 < rows_b ? 1 : 0)));
-        for (int kb = it.k0; kb < it.k1 && !*abort_flag;) {
+        const int lo = (int)(L.lo >> 7);
+        for (int at = it.k0; at < it.k1 && !*abort_flag;) {
+          const Run run(it, M, at);
           OperandRun a, b;
-          a.start(it.kind == kGram ? X : S, it.kind == kGram ? ne : me, ra, kb, is_mn(it.kind, false, it.I, kb), la);
-          b.start(it.kind == kSym ? S : X, it.kind == kSym ? me : ne, rb, kb, is_mn(it.kind, true, it.J, kb), lb);
-          for (const int e = run_end(it, kb); kb < e; ++kb) {
+          a.start((it.kind == kGram ? X : S) + (run.part == 2 ? lo : 0), it.kind == kGram ? ne : me, ra, run.kb, run.a_mn, la);
+          b.start((it.kind == kSym ? S : X) + (run.part == 1 ? lo : 0), it.kind == kSym ? me : ne, rb, run.kb, run.b_mn, lb);
+          for (int kb = run.kb; at < run.end; ++at, ++kb) {
             if (!mbar_wait(smem_u32(&empty[stage]), phase ^ 1, 3 * lim)) {
               record_timeout(p.status, abort_flag);
               break;
@@ -713,20 +773,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         if (it.kind == kStop) break;
         if (it.kind == kSum) continue;
-        const bool same = it.kind != kFull && it.I == it.J;
+        const OrthoMat& M = p.mat[it.mat];
+        const bool same = same_operand(it, M);
         if (!mbar_wait_cluster(smem_u32(&acc_empty[acc]), aphase ^ 1, 2 * lim)) {
           record_timeout(p.status, abort_flag);
           break;
         }
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(acc * 256);
-        for (int kb = it.k0; kb < it.k1 && !*abort_flag;) {
-          const bool a_mn = is_mn(it.kind, false, it.I, kb), b_mn = is_mn(it.kind, true, it.J, kb);
+        for (int at = it.k0; at < it.k1 && !*abort_flag;) {
+          const Run run(it, M, at);
+          const bool a_mn = run.a_mn, b_mn = run.b_mn;
           const uint64_t ad0 = a_mn ? mndesc : kdesc, bd0 = (b_mn ? mndesc : kdesc) + (same ? 0 : 2 * kOrthoBlk >> 4);
           const uint32_t as = a_mn ? 2048 >> 4 : 32 >> 4, bs = b_mn ? 2048 >> 4 : 32 >> 4;
           const uint32_t idesc = idesc_f16(256, 256, false, false, true) | (a_mn ? 1u << 15 : 0u) |
                                  (b_mn ? 1u << 16 : 0u);
-          for (const int e = run_end(it, kb); kb < e; ++kb) {
+          for (; at < run.end; ++at) {
             if (!mbar_wait_cluster(smem_u32(&full[stage]), phase, 2 * lim)) {
               record_timeout(p.status, abort_flag);
               break;
@@ -736,7 +798,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const uint64_t ad = ad0 + s, bd = bd0 + s;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              tc_mma_f16_pair(d, ad + (uint64_t)(kk * as), bd + (uint64_t)(kk * bs), idesc, kb > it.k0 || kk > 0);
+              tc_mma_f16_pair(d, ad + (uint64_t)(kk * as), bd + (uint64_t)(kk * bs), idesc, at > it.k0 || kk > 0);
             tc_commit_pair(smem_u32(&empty[stage]));
             if (++stage == kStages) {
               stage = 0;
@@ -781,7 +843,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (it.kind == kStop) break;
       const OrthoMat& M = p.mat[it.mat];
-      const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits);
+      const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits, M.precise);
       const bool full_kind = it.kind == kFull;
       const bool final_step = full_kind && it.step == p.steps - 1;
       const int ncb = full_kind ? M.nb : M.mb;  // block columns of the result
@@ -790,14 +852,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int chunks = !any ? 0 : bj0 + 1 < ncb ? 4 : 2;     // of 32 columns
       uint8_t* out = M.ws + (it.kind == kGram  ? L.a16
                              : it.kind == kSym ? L.b16
-                                               : L.x16 + ((it.step + 1) & 1) * (L.x32 / 2));
+                                               : L.x16 + ((it.step + 1) & 1) * (L.a16 / 2));
       out += ortho_block(bi, bj0, (ncb + 1) & ~1) * kOrthoBlk + (row & 32) * 128;
       const uint8_t* a16 = M.ws + L.a16 + ortho_block(bi, bj0, (M.mb + 1) & ~1) * kOrthoBlk + rr * 128;
       float4* x32 = reinterpret_cast<float4*>(M.ws + L.x32 + ((size_t)bi * M.nb + bj0) * (2 * kOrthoBlk)) + rr;
       const float mul = it.kind == kGram  ? kSa / (kSx * kSx)
                         : it.kind == kSym ? kC * kSb / (kSa * kSa)
                                           : 1.f / (kSx * kSb);
-      const TileOut o{p, M, it, out, a16, x32, mul, stage_w, chunks, rr, lane, row, bj0, full_kind, final_step};
+      const TileOut o{p, M, it, out, a16, x32, mul, stage_w, chunks, rr, lane, row, bj0, full_kind, final_step,
+                      M.precise ? L.lo : 0};
       // FP32 parts of a split sum: this warp's rows and columns, four columns a lane at a time
       float4* part = reinterpret_cast<float4*>(
                          M.ws + L.part +
@@ -828,6 +891,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const int ch = (it.split & 3) * 2;
           __stcg(reinterpret_cast<uint4*>(dst + ((ch ^ (rr & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
           __stcg(reinterpret_cast<uint4*>(dst + (((ch + 1) ^ (rr & 7)) << 4)), make_uint4(h[4], h[5], h[6], h[7]));
+          if (M.precise) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = low2(x[2 * j] * mul_a, x[2 * j + 1] * mul_a, h[j]);
+            __stcg(reinterpret_cast<uint4*>(dst + L.lo + ((ch ^ (rr & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
+            __stcg(reinterpret_cast<uint4*>(dst + L.lo + (((ch + 1) ^ (rr & 7)) << 4)), make_uint4(h[4], h[5], h[6], h[7]));
+          }
           fence_proxy_async_all();  // the operand copies read them
         }
         __syncwarp();

@@ -24,7 +24,8 @@ struct OrthoMat {
   int mb, nb;
   int part0, parts;   // its partial sums of squares
   int tall;
-  int splits, kper;   // X X^T: parts of the sum over n, and blocks of n in each
+  int precise;        // operands as pairs of binary16 (kOrthoPrecise): sums three times as long
+  int splits, kper;   // X X^T: parts of its sum, and blocks in each
   float scale;        // of the orthogonalised update in the weights' step
 };
 
@@ -60,18 +61,25 @@ __host__ __device__ inline int ortho_sym(int tiles) { return tiles * (tiles + 1)
 constexpr int kOrthoPart = 16384;
 constexpr int kOrthoSumItems = 8;
 
+// Matrices of at most one block of rows keep their operands as the sum of two binary16 copies, the
+// second of what the first's rounding left, and multiply high by high, high by low and low by high.
+// The roundings of single copies average out over many singular values; a few singular values can each
+// be several tenths of a percent off, and the products of so small a matrix cost nothing.
+constexpr int kOrthoPrecise = 1;
+
 struct OrthoLayout {
-  size_t x16, x32, a16, b16, part, bytes;
+  size_t x16, x32, a16, b16, lo, part, bytes;  // lo: from a binary16 grid to its low copy's
 };
-__host__ __device__ inline OrthoLayout ortho_layout(long long mb, long long nb, int splits) {
+__host__ __device__ inline OrthoLayout ortho_layout(long long mb, long long nb, int splits, int precise) {
   OrthoLayout l;
   const size_t me = (mb + 1) & ~1ll, ne = (nb + 1) & ~1ll;
   const size_t xb = me * ne * kOrthoBlk, ab = me * me * kOrthoBlk;
   l.x16 = 0;  // two buffers of xb bytes
-  l.x32 = 2 * xb;
-  l.a16 = l.x32 + (size_t)mb * nb * (2 * kOrthoBlk);
+  l.a16 = 2 * xb;
   l.b16 = l.a16 + ab;
-  l.part = l.b16 + ab;
+  l.lo = l.b16 + ab;
+  l.x32 = precise ? 2 * l.lo : l.lo;
+  l.part = l.x32 + (size_t)mb * nb * (2 * kOrthoBlk);
   l.bytes = l.part + (splits > 1 ? (size_t)ortho_sym(ortho_tiles((int)mb)) * splits * kOrthoSignals * kOrthoPart : 0);
   return l;
 }

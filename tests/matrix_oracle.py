@@ -11,15 +11,18 @@ def f16(x):
 
 
 def orthogonal(u, steps=5, copies=False):
-    """The definition; with copies, the products' operands rounded to binary16 as the library
-    states (X itself is not), in its scales."""
+    """The definition; with copies, the products' operands rounded as the library states (X itself
+    is not): to binary16 in its scales, or, of matrices of at most 64 rows or columns, to two of them."""
     a, b, c = COEFFS
     u = np.asarray(u, np.float64)
     size = np.sqrt((u * u).sum())
     if size == 0:
         return u
     x = (u.T if u.shape[0] > u.shape[1] else u) / size
-    r = (lambda v, s: f16(v * s) / s) if copies else (lambda v, s: v)
+    if copies and x.shape[0] <= 64:  # two copies: what the second leaves
+        r = lambda v, s: (f16(v * s) + f16(v * s - f16(v * s))) / s
+    else:
+        r = (lambda v, s: f16(v * s) / s) if copies else (lambda v, s: v)
     for _ in range(steps):
         h = r(x, 2.0 ** 15)
         s = r(h @ h.T, 2.0 ** 15)
