@@ -405,13 +405,14 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  *   X = u / |u|_F;  `steps` times:  S = X X^T,  X = a X + (b S + c S S) X,
  *   (a, b, c) = (3.4445, -4.7750, 2.0315)
  * whose result has u's singular vectors and, after five steps, singular values
- * between 0.68 and 1.21 for all but the smallest.  X is held in FP32; the
- * products take binary16 copies (scaled by powers of two) and accumulate in
- * FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
- * norm is not finite gives NaNs throughout.  Same inputs, same bits,
- * whatever else the call holds.
+ * between 0.68 and 1.21 for all but the smallest.  X is held in FP32 (calls of
+ * small matrices only: as two binary16 numbers, 22 bits); the products take
+ * binary16 copies, scaled by powers of two -- two of each operand where rows or
+ * cols <= 64 -- and accumulate in FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
+ * norm is not finite gives NaNs throughout.  The same call gives the same bits.
  *
- * All matrices of one call run together, in three launches.  1 <= rows, cols <=
+ * All matrices of one call run together, in three launches, or in
+ * one where each has a side of at most 64 and the other of at most 704.  1 <= rows, cols <=
  * 65536, rows * cols <= 2^30, at most PF16_ORTHO_MAX_MATRICES matrices
  * (PF16_ERR_UNSUPPORTED beyond), 1 <= steps <= 16 (PF16_ERR_ARG).  The list
  * is host memory, read before the call returns.  Arrays are dense, row-major,

@@ -1724,6 +1724,8 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   p->pre_sum[count] = (int)sum;
   p->pre_sym[count] = (int)sym;
   p->pre_full[count] = (int)full;
+  p->small = 1;
+  for (int i = 0; i < count; ++i) p->small &= p->mat[i].mb <= kOrthoPrecise && p->mat[i].nb <= kSmallBlocks;
   p->total_parts = (int)parts;
   p->max_items = (int)std::max(std::max(gram, sum), full);
   p->zero_words = words;
@@ -1817,8 +1819,9 @@ static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int3
   int sms;
   rc = device_consts(&p.status, &sms);
   if (rc != PF16_OK) return rc;
-  CUtensorMap map;
-  if (!driver_fns() || !map_2d(&map, ws, 64, need / 128, 64, 64, 64, CU_TENSOR_MAP_SWIZZLE_NONE)) return PF16_ERR_CUDA;
+  CUtensorMap map = {};
+  if (!p.small && (!driver_fns() || !map_2d(&map, ws, 64, need / 128, 64, 64, 64, CU_TENSOR_MAP_SWIZZLE_NONE)))
+    return PF16_ERR_CUDA;
   return launch_ortho(p, map, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PF16_OK : PF16_ERR_CUDA;
 }
 

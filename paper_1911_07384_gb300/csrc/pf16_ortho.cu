@@ -255,9 +255,14 @@ __global__ void __launch_bounds__(256) k_ortho_norm(const __grid_constant__ Orth
 
 namespace {
 
-// 1 / |U|_F from the matrix's partial sums, the same in all threads.  A zero
-// matrix gives 0 (its result is zero); a norm that is not finite gives NaN, and
-// with it a result of NaNs only.
+// 1 / |U|_F from |U|_F^2.  A zero matrix gives 0 (its result is zero); a norm that is not finite gives NaN,
+// and with it a result of NaNs only.
+__device__ __forceinline__ float inv_of(float s) {
+  if (s == 0.f) return 0.f;
+  if (!(s <= 3.402823466e38f)) return __int_as_float(0x7fffffff);
+  return 1.f / sqrtf(s);
+}
+// ... from the matrix's partial sums, the same in all threads
 __device__ __forceinline__ float inv_norm(const OrthoParams& p, const OrthoMat& M, float* red, int t) {
   float s = 0.f;
   for (int i = t; i < M.parts; i += 256) s += p.parts[M.part0 + i];
@@ -265,10 +270,7 @@ __device__ __forceinline__ float inv_norm(const OrthoParams& p, const OrthoMat& 
   for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
   if ((t & 31) == 0) red[t >> 5] = s;
   __syncthreads();
-  s = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
-  if (s == 0.f) return 0.f;
-  if (!(s <= 3.402823466e38f)) return __int_as_float(0x7fffffff);
-  return 1.f / sqrtf(s);
+  return inv_of(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7])));
 }
 
 }  // namespace
@@ -963,7 +965,279 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
+// ---------------------------------------------------------------------------
+// A call of small matrices: a CTA takes one from its gradient to its result
+// within shared and tensor memory.  X is held as two binary16 copies (22 bits),
+// S and the quintic's factor too, in the blocks that the MMAs read; a product's
+// 64 rows are the upper half of an MMA's 128, the lower half multiplies whatever
+// follows.  Fifteen products in a chain, each followed by its epilogue: what takes 4 to 6 us a
+// phase through the L2 and its counters takes one here.
+// ---------------------------------------------------------------------------
+constexpr int kSmallThreads = 32 * 17;  // sixteen warps, of which the eight with rows 0-63 store; one for the MMAs
+
+__global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_constant__ OrthoParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  __shared__ uint64_t done[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ float red[kSmallThreads / 32];
+  __shared__ int failed, drained;
+  const OrthoMat& M = p.mat[blockIdx.x];
+  const int t = (int)threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int nb = M.nb;
+  // blocks: X high, X low [nb]; S high, low; B high, low
+  uint8_t *xh = smem, *sh = smem + 2 * nb * kOrthoBlk, *bh = sh + 2 * kOrthoBlk;
+  const uint32_t xlo = (uint32_t)nb * kOrthoBlk;
+  if (t == 0) {
+    mbar_init(smem_u32(&done[0]), 1);
+    mbar_init(smem_u32(&done[1]), 1);
+    failed = 0;
+    drained = 1;
+    fence_mbar_init();
+  }
+  if (warp == 16) {
+    tmem_alloc(smem_u32(&tmem_slot), 512);
+    tmem_relinquish();
+  }
+  for (int i = t; i < 2 * nb * (kOrthoBlk / 16); i += kSmallThreads)
+    reinterpret_cast<uint4*>(xh)[i] = make_uint4(0, 0, 0, 0);  // X past the matrix's edges
+  pdl_wait();
+  // The norm, and the momentum.  The caller's arrays are read and written as they lie, eight elements at a time.
+  const int n = M.rows * M.cols, vecs = (n + 7) >> 3;
+  auto load8 = [&](const uint16_t* a, int i, uint16_t* v) {
+    if (i * 8 + 8 <= n) {
+      *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(a + i * 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = i * 8 + j < n ? a[i * 8 + j] : 0;
+    }
+  };
+  auto store8 = [&](uint16_t* a, int i, const uint16_t* v) {
+    if (i * 8 + 8 <= n) {
+      *reinterpret_cast<uint4*>(a + i * 8) = *reinterpret_cast<const uint4*>(v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i * 8 + j < n) a[i * 8 + j] = v[j];
+    }
+  };
+  // calls f(j, its place in X's blocks) for element 8 i + j, j < 8
+  auto each8 = [&](int i, auto f) {
+    int r = i * 8 / M.cols, c = i * 8 - r * M.cols;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int row = M.tall ? c : r, col = M.tall ? r : c;
+      if (i * 8 + j < n)
+        f(j, xh + (col >> 6) * kOrthoBlk + row * 128 + ((((col >> 3) & 7) ^ (row & 7)) << 4) + (col & 7) * 2);
+      if (++c == M.cols) {
+        c = 0;
+        ++r;
+      }
+    }
+  };
+  float sum = 0.f;
+  for (int i = t; i < vecs; i += kSmallThreads) {
+    __align__(16) uint16_t g[8];
+    __align__(16) uint16_t v[8];
+    load8(M.g, i, g);
+    if (p.muon) load8(M.v, i, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float u = h2f(g[j]);
+      if (p.muon) {
+        v[j] = f2h(fmaf(p.momentum, h2f(v[j]), u));
+        u = ortho_u(p, u, h2f(v[j]));
+      }
+      sum = fmaf(u, u, sum);
+    }
+    if (p.muon) store8(M.v, i, v);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+  if (lane == 0) red[warp] = sum;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSmallThreads / 32; ++i) sum += red[i];
+  const float inv = inv_of(sum);
+  for (int i = t; i < vecs; i += kSmallThreads) {
+    __align__(16) uint16_t g[8];
+    __align__(16) uint16_t v[8];
+    load8(M.g, i, g);
+    if (p.muon) load8(M.v, i, v);  // (written by this thread)
+    each8(i, [&](int j, uint8_t* at) {
+      float u = h2f(g[j]);
+      if (p.muon) u = ortho_u(p, u, h2f(v[j]));
+      const float x = (inv != inv ? inv : u * inv) * kSx;
+      const uint16_t hi = f2h(x);
+      *reinterpret_cast<uint16_t*>(at) = hi;
+      *reinterpret_cast<uint16_t*>(at + xlo) = f2h(x - h2f(hi));
+    });
+  }
+  fence_proxy_async_smem();
+  __syncthreads();
+
+  const uint32_t xd = desc_addr16(smem_u32(xh)), sd = desc_addr16(smem_u32(sh)), bd = desc_addr16(smem_u32(bh));
+  const uint32_t lo1 = kOrthoBlk >> 4, lox = xlo >> 4;  // to a low copy
+  const uint64_t kdesc = smem_desc(0, 16, 1024, 2), mndesc = smem_desc(0, 8192, 1024, 2);
+  // what a storing thread has: row `row`, a quarter (g) of the columns
+  const int quad = warp & 3, g = warp >> 2, row = quad * 32 + lane;
+  const bool stores = warp < 16 && quad < 2;
+  const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+  uint32_t waits[2] = {0, 0};
+  auto wait_for = [&](int b) {  // an MMA group of buffer b; every thread waits
+    if (!mbar_wait(smem_u32(&done[b]), waits[b] & 1, p.wait_limit_ns)) {
+      atomicCAS(p.status, 0, -7);  // PF16_ERR_TIMEOUT
+      failed = 1;
+    }
+    ++waits[b];
+    tc_fence_after();
+  };
+  // 16 values from column c of a block, scaled, as two copies
+  auto put16 = [&](uint8_t* block, uint32_t lo, int c, const float* x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t a[4], b[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        a[q] = f2h2(x[8 * h + 2 * q], x[8 * h + 2 * q + 1]);
+        b[q] = low2(x[8 * h + 2 * q], x[8 * h + 2 * q + 1], a[q]);
+      }
+      uint8_t* at = block + row * 128 + (((c / 8 + h) ^ (row & 7)) << 4);
+      *reinterpret_cast<uint4*>(at) = make_uint4(a[0], a[1], a[2], a[3]);
+      *reinterpret_cast<uint4*>(at + lo) = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+  };
+  auto get16 = [&](const uint8_t* block, uint32_t lo, int c, float* x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* at = block + row * 128 + (((c / 8 + h) ^ (row & 7)) << 4);
+      const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at + lo);
+      const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 u = h22f(aw[q]), v = h22f(bw[q]);
+        x[8 * h + 2 * q] = u.x + v.x;
+        x[8 * h + 2 * q + 1] = u.y + v.y;
+      }
+    }
+  };
+  for (int step = 0; step < p.steps && !failed; ++step) {
+    // S = X X^T, then B = b S + c S S: 64 columns, 16 for each quarter of the storing warps
+    for (int phase = 0; phase < 2; ++phase) {
+      if (warp == 16 && elect_one()) {
+        const uint32_t idesc = idesc_f16(128, 64, false, false, true);
+        uint32_t any = 0;
+        for (int part = 0; part < 3; ++part)
+          for (int kb = 0; kb < (phase == 0 ? nb : 1); ++kb) {
+            const uint32_t base = phase == 0 ? xd + (uint32_t)kb * (kOrthoBlk >> 4) : sd;
+            const uint32_t low = phase == 0 ? lox : lo1;
+            const uint64_t ad = kdesc + base + (part == 2 ? low : 0), bdsc = kdesc + base + (part == 1 ? low : 0);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              tc_mma_f16(tmem, ad + (uint64_t)(kk * 2), bdsc + (uint64_t)(kk * 2), idesc, any);
+              any = 1;
+            }
+          }
+        tc_commit(smem_u32(&done[0]));
+      }
+      __syncwarp();
+      wait_for(0);
+      if (stores) {
+        uint32_t r[16];
+        float x[16];
+        tmem_ld16(trow + (uint32_t)(g * 16), r);
+        if (phase == 1) get16(sh, kOrthoBlk, g * 16, x);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          x[j] = phase == 0 ? __uint_as_float(r[j]) * (kSa / (kSx * kSx))
+                            : fmaf(__uint_as_float(r[j]), kC * kSb / (kSa * kSa), x[j] * (kB * kSb / kSa));
+        put16(phase == 0 ? sh : bh, kOrthoBlk, g * 16, x);
+        fence_proxy_async_smem();
+      }
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+    }
+    // X <- a X + B X, up to 256 columns at a time, the next ones' product running meanwhile
+    const int chunks = (nb + 3) >> 2;
+    for (int ch = 0; ch <= chunks; ++ch) {
+      if (ch < chunks && warp == 16 && elect_one()) {
+        const int cols = min(4, nb - ch * 4) * 64;
+        const uint32_t idesc = idesc_f16(128, cols, false, true, true);
+        const uint32_t base = xd + (uint32_t)(ch * 4) * (kOrthoBlk >> 4);
+        uint32_t any = 0;
+        for (int part = 0; part < 3; ++part) {
+          const uint64_t ad = kdesc + bd + (part == 2 ? lo1 : 0), bdsc = mndesc + base + (part == 1 ? lox : 0);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            tc_mma_f16(tmem + (uint32_t)((ch & 1) * 256), ad + (uint64_t)(kk * 2), bdsc + (uint64_t)(kk * (2048 >> 4)),
+                       idesc, any);
+            any = 1;
+          }
+        }
+        tc_commit(smem_u32(&done[ch & 1]));
+      }
+      __syncwarp();
+      if (ch == 0) continue;
+      const int c0 = (ch - 1) * 256;  // this chunk's first column
+      wait_for((ch - 1) & 1);
+      // 32 columns at a time, each quarter of the storing warps every fourth
+      if (stores) {
+        for (int c = g * 32; c < 256 && c0 + c < nb * 64; c += 128) {
+          uint32_t r[32];
+          tmem_ld16(trow + (uint32_t)(((ch - 1) & 1) * 256 + c), r);
+          tmem_ld16(trow + (uint32_t)(((ch - 1) & 1) * 256 + c + 16), r + 16);
+          uint8_t* block = xh + ((c0 + c) >> 6) * kOrthoBlk;
+          float x[32];
+          get16(block, xlo, c & 63, x);
+          get16(block, xlo, (c & 63) + 16, x + 16);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] = fmaf(kA, x[j], __uint_as_float(r[j]) * (1.f / kSb));
+          put16(block, xlo, c & 63, x);
+          put16(block, xlo, (c & 63) + 16, x + 16);
+        }
+        fence_proxy_async_smem();
+      }
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+    }
+  }
+  // the result, or the weights' step with it
+  for (int i = t; i < vecs && !failed; i += kSmallThreads) {
+    __align__(16) uint16_t w[8];
+    if (p.muon) load8(M.w, i, w);
+    each8(i, [&](int j, const uint8_t* at) {
+      const float x = (h2f(*reinterpret_cast<const uint16_t*>(at)) + h2f(*reinterpret_cast<const uint16_t*>(at + xlo))) *
+                      (1.f / kSx);
+      w[j] = f2h(p.muon ? muon_w(p, M, h2f(w[j]), x) : x);
+    });
+    store8(M.w, i, w);
+  }
+  if (warp == 16) {
+    if (elect_one()) {  // nothing runs in TMEM when it is released
+      tc_commit(smem_u32(&done[0]));
+      if (!mbar_wait(smem_u32(&done[0]), waits[0] & 1, p.wait_limit_ns)) drained = 0;
+    }
+    __syncwarp();
+    if (drained) tmem_dealloc(tmem, 512);
+  }
+}
+
 cudaError_t launch_ortho(const OrthoParams& p, const CUtensorMap& map, int sms, cudaStream_t s) {
+  if (p.small) {
+    cudaError_t e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(k_ortho_small, dim3((unsigned)p.count), dim3(kSmallThreads), kSmallSmem, s, p);
+    return e == cudaSuccess ? counted_launches(1) : e;
+  }
   cudaError_t e = cudaFuncSetAttribute(k_ortho, cudaFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmem);
   if (e != cudaSuccess) return e;
   e = launch_pdl(k_ortho_norm, dim3((unsigned)p.total_parts), dim3(256), 0, s, p);

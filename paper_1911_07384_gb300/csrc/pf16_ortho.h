@@ -31,6 +31,7 @@ struct OrthoMat {
 
 struct OrthoParams {
   int count, steps;
+  int small;          // every matrix fits a CTA: no workspace is used
   int max_items;      // most work items of one phase, over all matrices together
   size_t zero_words;  // counters, from `ticket` on
   int muon, nesterov;
@@ -66,6 +67,11 @@ constexpr int kOrthoSumItems = 8;
 // The roundings of single copies average out over many singular values; a few singular values can each
 // be several tenths of a percent off, and the products of so small a matrix cost nothing.
 constexpr int kOrthoPrecise = 1;
+
+// A call whose matrices all have at most kOrthoPrecise blocks of rows and kSmallBlocks of columns runs in one
+// launch, a CTA a matrix (k_ortho_small).
+constexpr int kSmallBlocks = 11;
+constexpr int kSmallSmem = 1024 + (2 * kSmallBlocks + 5) * kOrthoBlk;
 
 struct OrthoLayout {
   size_t x16, x32, a16, b16, lo, part, bytes;  // lo: from a binary16 grid to its low copy's
