@@ -583,7 +583,6 @@ struct TileOut {
                                         ((((c & 1) * 4 + h) ^ (rr & 7)) << 4)),
                make_uint4(l[0], l[1], l[2], l[3]));
       }
-      fence_proxy_async_all();  // the operand copies read them
     }
 #pragma unroll
     for (int h = 0; h < 4; ++h)
@@ -591,7 +590,10 @@ struct TileOut {
                    make_uint4(f2h2(f[8 * h], f[8 * h + 1]), f2h2(f[8 * h + 2], f[8 * h + 3]),
                               f2h2(f[8 * h + 4], f[8 * h + 5]), f2h2(f[8 * h + 6], f[8 * h + 7])));
     if (c & 1) {
-      fence_proxy_async_smem();
+      if (lo)
+        fence_proxy_async_all();  // the operand copies read what was stored directly
+      else
+        fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         bulk_store_1d(out + (c >> 1) * (2 * kOrthoBlk), stage_w, 4096);
@@ -870,7 +872,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                      lane;
       constexpr int kNext = kOrthoSignals * kOrthoPart / 16;  // to the next part
       if (it.kind == kSum) {
-        if (it.split * 16 < chunks * 32) {
+        constexpr int kCols = 8 / kOrthoSumItems;  // of 16 columns
+        for (int g = it.split * kCols; g < (it.split + 1) * kCols && g * 16 < chunks * 32; ++g) {
           float x[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) x[j] = 0.f;
@@ -878,29 +881,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int s = 0; s < M.splits; ++s) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float4 f = __ldcg(part + s * kNext + (it.split * 4 + j) * 32);
+              const float4 f = __ldcg(part + s * kNext + (g * 4 + j) * 32);
               x[4 * j] += f.x;
               x[4 * j + 1] += f.y;
               x[4 * j + 2] += f.z;
               x[4 * j + 3] += f.w;
             }
           }
-          const float mul_a = kSa / (kSx * kSx);
           uint32_t h[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) h[j] = f2h2(x[2 * j] * mul_a, x[2 * j + 1] * mul_a);
-          uint8_t* dst = const_cast<uint8_t*>(a16) + (it.split >> 2) * (2 * kOrthoBlk);
-          const int ch = (it.split & 3) * 2;
-          __stcg(reinterpret_cast<uint4*>(dst + ((ch ^ (rr & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
-          __stcg(reinterpret_cast<uint4*>(dst + (((ch + 1) ^ (rr & 7)) << 4)), make_uint4(h[4], h[5], h[6], h[7]));
+          for (int j = 0; j < 16; ++j) x[j] *= kSa / (kSx * kSx);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) h[j] = f2h2(x[2 * j], x[2 * j + 1]);
+          uint8_t* dst = const_cast<uint8_t*>(a16) + (g >> 2) * (2 * kOrthoBlk);
+          const int p0 = (((g & 3) * 2) ^ (rr & 7)) << 4, p1 = (((g & 3) * 2 + 1) ^ (rr & 7)) << 4;
+          __stcg(reinterpret_cast<uint4*>(dst + p0), make_uint4(h[0], h[1], h[2], h[3]));
+          __stcg(reinterpret_cast<uint4*>(dst + p1), make_uint4(h[4], h[5], h[6], h[7]));
           if (M.precise) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = low2(x[2 * j] * mul_a, x[2 * j + 1] * mul_a, h[j]);
-            __stcg(reinterpret_cast<uint4*>(dst + L.lo + ((ch ^ (rr & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
-            __stcg(reinterpret_cast<uint4*>(dst + L.lo + (((ch + 1) ^ (rr & 7)) << 4)), make_uint4(h[4], h[5], h[6], h[7]));
+            for (int j = 0; j < 8; ++j) h[j] = low2(x[2 * j], x[2 * j + 1], h[j]);
+            __stcg(reinterpret_cast<uint4*>(dst + L.lo + p0), make_uint4(h[0], h[1], h[2], h[3]));
+            __stcg(reinterpret_cast<uint4*>(dst + L.lo + p1), make_uint4(h[4], h[5], h[6], h[7]));
           }
-          fence_proxy_async_all();  // the operand copies read them
         }
+        fence_proxy_async_all();  // the operand copies read them
         __syncwarp();
         if (lane == 0) red_release_add(p.done + it.mat, 1u);
         continue;

@@ -57,8 +57,8 @@ constexpr int kOrthoPairs = 76;      // of SMs
 __host__ __device__ inline int ortho_tiles(int blocks) { return (blocks + 3) >> 2; }
 __host__ __device__ inline int ortho_sym(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Split sums of X X^T: FP32 parts [tile][split][CTA of the pair][warp], 16 KB each, added in items of
-// 16 of each warp's 128 columns.
+// Split sums of X X^T: FP32 parts [tile][split][CTA of the pair][warp], 16 KB each, added in items
+// of a share of each warp's 128 columns.
 constexpr int kOrthoPart = 16384;
 constexpr int kOrthoSumItems = 8;
 
