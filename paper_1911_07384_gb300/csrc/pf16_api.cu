@@ -1679,7 +1679,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
   const size_t words = 4 + (size_t)count;
-  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0;
+  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0, wide = 0;
   for (int i = 0; i < count; ++i) {
     const OrthoEntry& s = e[order[i]];
     OrthoMat& m = p->mat[i];
@@ -1707,17 +1707,24 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     m.splits = (int)std::min<long long>(8, std::max<long long>(1, terms / share));
     m.kper = cdiv(terms, m.splits);
     m.splits = cdiv(terms, m.kper);
-    const int mt = ortho_tiles(m.mb), nt = ortho_tiles(m.nb), tri = ortho_sym(mt);
+    const int mt = ortho_tiles(m.mb), tri = ortho_sym(mt);
     p->pre_pack[i] = (int)pack;
     p->pre_gram[i] = (int)gram;
     p->pre_sum[i] = (int)sum;
     p->pre_sym[i] = (int)sym;
-    p->pre_full[i] = (int)full;
     pack += (long long)m.mb * m.nb;
     gram += (long long)tri * m.splits;
     if (m.splits > 1) sum += (long long)tri * kOrthoSumItems;
     sym += tri;
-    full += (long long)mt * nt;
+    wide += (long long)mt * cdiv(m.nb, 4);
+  }
+  // The full product's tiles are 256 columns wide, or 128 where there are so few that the time of one
+  // counts, most of it its epilogue's, which reads and writes X (256, 128 wide: 512 x 512 200, 178 us;
+  // 256 x 2304 232, 201; 1000 x 2048, 32 tiles of 256, 249, 257).
+  p->full_blocks = wide >= kOrthoPairs / 4 ? 4 : 2;
+  for (int i = 0; i < count; ++i) {
+    p->pre_full[i] = (int)full;
+    full += (long long)ortho_tiles(p->mat[i].mb) * cdiv(p->mat[i].nb, p->full_blocks);
   }
   p->pre_pack[count] = (int)pack;
   p->pre_gram[count] = (int)gram;

@@ -171,7 +171,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     it.k1 = ortho_sum(p.mat[it.mat].mb, p.mat[it.mat].precise);
   }
   const OrthoMat& M = p.mat[it.mat];
-  const int mt = ortho_tiles(M.mb), nt = ortho_tiles(M.nb);
+  const int mt = ortho_tiles(M.mb), nt = (M.nb + p.full_blocks - 1) / p.full_blocks;
   const uint32_t tri = (uint32_t)ortho_sym(mt), gram = tri * (uint32_t)M.splits;
   const uint32_t sum = M.splits > 1 ? tri * kOrthoSumItems : 0;
   uint32_t before = (uint32_t)it.step * (gram + sum + tri + (uint32_t)(mt * nt));
@@ -466,23 +466,21 @@ __device__ __forceinline__ void load_block(const CUtensorMap* map, uint32_t dst,
       : "memory");
 }
 
-// 128 rows of an operand, two blocks, for block after block along the sum.  Positions count rows of
+// A CTA's rows of an operand, two blocks (or one), for block after block along the sum.  Positions count rows of
 // 128 bytes in the workspace, 64 a block.
 struct OperandRun {
   int at, second, even, odd;  // to the second block; to the next ones from an even block, from an odd one
-  bool live;
-  __device__ __forceinline__ void start(int grid, int pitch, int row, int kb, bool mn, bool live_) {
-    live = live_;
+  int blocks;
+  __device__ __forceinline__ void start(int grid, int pitch, int row, int kb, bool mn, int blocks_) {
+    blocks = blocks_;
     at = grid + 64 * (int)(mn ? ortho_block(kb, row, pitch) : ortho_block(row, kb, pitch));
     second = mn ? 128 : 64;
     even = mn ? 64 : 128;
     odd = mn ? 64 * (2 * pitch - 1) : 128;
   }
   __device__ __forceinline__ void load(const CUtensorMap* map, uint32_t dst, uint32_t bar, int kb) {
-    if (live) {
-      load_block(map, dst, bar, at);
-      load_block(map, dst + kOrthoBlk, bar, at + second);
-    }
+    if (blocks > 0) load_block(map, dst, bar, at);
+    if (blocks > 1) load_block(map, dst + kOrthoBlk, bar, at + second);
     at += (kb & 1) ? odd : even;
   }
 };
@@ -710,13 +708,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int X = base + (int)((L.x16 + (it.step & 1) * (L.a16 / 2)) >> 7);
         const int S = base + (int)((it.kind == kFull ? L.b16 : L.a16) >> 7);  // the symmetric operand
         const int me = (M.mb + 1) & ~1, ne = (M.nb + 1) & ~1;
-        const int ra = it.I * 4 + (int)rank * 2, rb = it.J * 4 + (int)rank * 2;  // first row of blocks
+        const int half_b = it.kind == kFull ? p.full_blocks / 2 : 2;
+        const int ra = it.I * 4 + (int)rank * 2, rb = (it.J * 2 + (int)rank) * half_b;  // first row of blocks
         const bool same = same_operand(it, M);
         const int rows_b = it.kind == kFull ? M.nb : M.mb;
-        const bool la = ra < M.mb, lb = !same && rb < rows_b;
+        const int la = ra < M.mb ? 2 : 0, lb = !same && rb < rows_b ? half_b : 0;
         // both CTAs' bytes (the first rows of a tile, the leading CTA's, are never past the edge)
-        const uint32_t bytes = 2 * kOrthoBlk * (uint32_t)(1 + (it.I * 4 + 2 < M.mb ? 1 : 0) +
-                                                          (same ? 0 : 1 + (it.J * 4 + 2 < rows_b ? 1 : 0)));
+        const uint32_t bytes = kOrthoBlk * (uint32_t)((it.I * 4 + 2 < M.mb ? 4 : 2) +
+                                                      (same ? 0 : ((it.J * 2 + 1) * half_b < rows_b ? 2 : 1) * half_b));
         const int lo = (int)(L.lo >> 7);
         for (int at = it.k0; at < it.k1 && !*abort_flag;) {
           const Run run(it, M, at);
@@ -764,6 +763,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int stage = 0, slot = 0, acc = 0;
       uint32_t phase = 0, rphase = 0, aphase = 0;
       const uint64_t kdesc = smem_desc(0, 16, 1024, 2), mndesc = smem_desc(0, 8192, 1024, 2);
+      const uint32_t idesc_full = idesc_f16(256, p.full_blocks * 64, false, false, true);
       while (!*abort_flag) {
         if (!mbar_wait_cluster(smem_u32(&item_full[slot]), rphase, 4 * lim)) {
           record_timeout(p.status, abort_flag);
@@ -790,7 +790,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const bool a_mn = run.a_mn, b_mn = run.b_mn;
           const uint64_t ad0 = a_mn ? mndesc : kdesc, bd0 = (b_mn ? mndesc : kdesc) + (same ? 0 : 2 * kOrthoBlk >> 4);
           const uint32_t as = a_mn ? 2048 >> 4 : 32 >> 4, bs = b_mn ? 2048 >> 4 : 32 >> 4;
-          const uint32_t idesc = idesc_f16(256, 256, false, false, true) | (a_mn ? 1u << 15 : 0u) |
+          const uint32_t idesc = (it.kind == kFull ? idesc_full : idesc_f16(256, 256, false, false, true)) | (a_mn ? 1u << 15 : 0u) |
                                  (b_mn ? 1u << 16 : 0u);
           for (; at < run.end; ++at) {
             if (!mbar_wait_cluster(smem_u32(&full[stage]), phase, 2 * lim)) {
@@ -827,7 +827,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     const int ew = warp - 2, lane = (int)threadIdx.x & 31, quad = warp & 3;
     const int row = (int)rank * 128 + quad * 32 + lane;  // of the tile
-    const int half = ew >> 2;                            // its columns, 128 of them, 32 at a time
+    const int half = ew >> 2;                            // its columns, 128 or 64 of them, 32 at a time
     const int rr = row & 63;
     const uint32_t far_item = map_rank(smem_u32(&item_empty[0]), 0), far_acc = map_rank(smem_u32(&acc_empty[0]), 0);
     const uint32_t stage_w = smem_u32(staging + ew * 4096);  // this warp's 32 rows of a block
@@ -851,9 +851,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const bool full_kind = it.kind == kFull;
       const bool final_step = full_kind && it.step == p.steps - 1;
       const int ncb = full_kind ? M.nb : M.mb;  // block columns of the result
-      const int bi = it.I * 4 + (row >> 6), bj0 = it.J * 4 + half * 2;
+      const int half_b = full_kind ? p.full_blocks / 2 : 2;  // blocks of this warp's columns
+      const int bi = it.I * 4 + (row >> 6), bj0 = (it.J * 2 + half) * half_b;
       const bool any = bi < M.mb && bj0 < ncb;                 // the same in the whole warp
-      const int chunks = !any ? 0 : bj0 + 1 < ncb ? 4 : 2;     // of 32 columns
+      const int chunks = !any ? 0 : half_b == 2 && bj0 + 1 < ncb ? 4 : 2;  // of 32 columns
       uint8_t* out = M.ws + (it.kind == kGram  ? L.a16
                              : it.kind == kSym ? L.b16
                                                : L.x16 + ((it.step + 1) & 1) * (L.a16 / 2));
@@ -919,7 +920,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         break;
       }
       tc_fence_after();
-      const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * 128);
+      const uint32_t tacc = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * half_b * 64);
       if (it.kind == kGram && M.splits > 1) {
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {

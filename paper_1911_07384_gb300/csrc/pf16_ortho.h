@@ -32,6 +32,7 @@ struct OrthoMat {
 struct OrthoParams {
   int count, steps;
   int small;          // every matrix fits a CTA: no workspace is used
+  int full_blocks;    // columns of the full product's tiles, in blocks: 4 or 2
   int max_items;      // most work items of one phase, over all matrices together
   size_t zero_words;  // counters, from `ticket` on
   int muon, nesterov;
