@@ -229,3 +229,39 @@ def test_captured_and_replayed():
             assert pf16.sync_status(st) == 0
             qq, ss = mo.quantize(a)
             check_linear(qq, ss.astype(np.float32), w, sw, b, y.cpu().numpy())
+
+
+def test_offsets_past_32_bits():
+    """Arrays of more than 2^32 bytes: rows near their ends, found by their own values."""
+    import torch
+
+    m, k, n = 70001, 32768, 40
+    x = torch.zeros(m, k, dtype=torch.float16, device="cuda")
+    rows = [0, 32767, 65535, 65536, 70000]
+    rng = np.random.default_rng(3)
+    some = rng.standard_normal((len(rows), k)).astype(np.float16)
+    x[rows] = dev(some)
+    q, s = torch.full((m, k), 7, dtype=torch.int8, device="cuda"), torch.full((m,), 3.0, device="cuda")
+    pf16.quantize_i8(x, q, s, m, k)
+    assert pf16.sync_status() == 0
+    want, scale = mo.quantize(some)
+    assert np.array_equal(q[rows].cpu().numpy(), want) and np.array_equal(s[rows].cpu().numpy(), scale.astype(np.float32))
+    assert int(q.count_nonzero()) == np.count_nonzero(want) and int(s.count_nonzero()) == len(rows)
+    del x
+    w, sw = rng.integers(-128, 128, (n, k)).astype(np.int8), np.full(n, 1e-4, np.float32)
+    y = torch.empty(m, n, dtype=torch.float16, device="cuda")
+    pf16.linear_i8(q, s, dev(w), dev(sw), None, y, m, n, k)
+    assert pf16.sync_status() == 0
+    check_linear(want, scale.astype(np.float32), w, sw, None, y[rows].cpu().numpy())
+    assert int(y.count_nonzero()) <= len(rows) * n
+    del q, y
+    # and of the output
+    m, n, k = 66001, 33000, 16
+    xq, wq = (rng.integers(-128, 128, (r, k)).astype(np.int8) for r in (m, n))
+    sx, sw = (np.full(r, 1e-2, np.float32) for r in (m, n))
+    b = rng.standard_normal(n).astype(np.float16)
+    y = torch.empty(m, n, dtype=torch.float16, device="cuda")
+    pf16.linear_i8(dev(xq), dev(sx), dev(wq), dev(sw), dev(b), y, m, n, k)
+    assert pf16.sync_status() == 0
+    rows = [0, 32768, 65087, 65088, 66000]
+    check_linear(xq[rows], sx[rows], wq, sw, b, y[rows].cpu().numpy())

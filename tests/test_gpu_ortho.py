@@ -86,9 +86,16 @@ def test_spectra(rows, cols, kind):
     check(ortho([g])[0], g)
 
 
-@pytest.mark.parametrize("steps", [1, 2, 3, 7])
-def test_steps(steps):
-    g = gradient(np.random.default_rng(steps), 100, 140)
+@pytest.mark.parametrize("rows,cols", [(1, 65536), (65536, 1), (2, 60001), (3, 9000), (130, 5000)])
+def test_long_and_thin(rows, cols):
+    g = gradient(np.random.default_rng(rows), rows, cols)
+    check(ortho([g])[0], g)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 7, 16])
+@pytest.mark.parametrize("rows,cols", [(100, 140), (50, 70)])
+def test_steps(rows, cols, steps):
+    g = gradient(np.random.default_rng(steps), rows, cols)
     check(ortho([g], steps)[0], g, steps)
 
 
@@ -106,15 +113,16 @@ def test_many_matrices_in_one_call():
         assert np.array_equal(ortho([gs[i]])[0], got[i])
 
 
-def test_values_at_the_edges():
+@pytest.mark.parametrize("rows,cols", [(70, 90), (40, 60), (60, 800)])
+def test_values_at_the_edges(rows, cols):
     rng = np.random.default_rng(2)
-    g = gradient(rng, 70, 90)
-    zero = np.zeros((70, 90), np.float16)
+    g = gradient(rng, rows, cols)
+    zero = np.zeros((rows, cols), np.float16)
     one = zero.copy()
     one[3, 5] = -6e-8  # a single subnormal element: singular value one
     bad = [g.copy() for _ in range(3)]
-    bad[0][1, 2], bad[1][69, 89], bad[2][0, 0] = np.inf, np.nan, -np.inf
-    big = np.full((70, 90), 65504, np.float16)
+    bad[0][1, 2], bad[1][-1, -1], bad[2][0, 0] = np.inf, np.nan, -np.inf
+    big = np.full((rows, cols), 65504, np.float16)
     got = ortho([g, zero, one, big, *bad])
     check(got[0], g)
     assert not got[1].any()
@@ -193,8 +201,32 @@ def test_two_calls_at_once():
         assert np.array_equal(o.cpu().numpy().astype(np.float64), a)
 
 
+def test_beside_other_work_on_the_gpu():
+    """Products of another stream hold most of the SMs while the phases wait for one another."""
+    import torch
+
+    rng = np.random.default_rng(21)
+    gs = [gradient(rng, 500, 700), gradient(rng, 300, 200)]
+    alone = ortho(gs)
+    ts, outs = [dev(g) for g in gs], [torch.zeros(g.shape, dtype=torch.float16, device="cuda") for g in gs]
+    mats = pf16.ortho_list([(t, o, *g.shape) for t, o, g in zip(ts, outs, gs)])
+    ws = space(pf16.ortho_workspace_size(mats))
+    a = torch.randn(4096, 4096, device="cuda", dtype=torch.float16)
+    other, mine = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        with torch.cuda.stream(other):
+            for _ in range(4):
+                a @ a
+        pf16.orthogonalize(mats, ws, stream=mine)
+    torch.cuda.synchronize()
+    assert pf16.sync_status(mine) == 0
+    for o, e in zip(outs, alone):
+        assert np.array_equal(o.cpu().numpy().astype(np.float64), e)
+
+
 @pytest.mark.parametrize("nesterov", [False, True])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (64, 147), (65, 64), (300, 130), (128, 1152)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (64, 147), (65, 64), (300, 130), (128, 1152), (257, 90), (64, 1000)])
 def test_muon(rows, cols, nesterov):
     rng = np.random.default_rng(rows + cols)
     w, v, g = ((rng.standard_normal((rows, cols)) * s).astype(np.float16) for s in (0.1, 0.05, 0.02))
