@@ -406,14 +406,19 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  *   (a, b, c) = (3.4445, -4.7750, 2.0315)
  * whose result has u's singular vectors and, after five steps, singular values
  * between 0.68 and 1.21 for all but the smallest.  X is held in FP32 (calls of
- * small matrices only: as two binary16 numbers, 22 bits); the products take
- * binary16 copies, scaled by powers of two -- two of each operand where rows or
- * cols <= 64 -- and accumulate in FP32; the result is rounded once.  A zero matrix gives zeros; a matrix whose
- * norm is not finite gives NaNs throughout.  The same call gives the same bits.
+ * small matrices only: as two binary16 numbers, 22 bits).  The products take
+ * binary16 copies of their operands, scaled by powers of two, and accumulate
+ * in FP32: two copies of each, 22 bits, in the last three steps, and in every
+ * step where rows or cols <= 64; one copy elsewhere.  The result is rounded
+ * once.  That rounding is most of its error (2.1e-4 of the norm), unless the
+ * matrix has a small rank: of rank 1, 9e-4.  A zero matrix gives zeros; a
+ * matrix whose norm is not finite gives NaNs throughout.  The same call gives
+ * the same bits.
  *
- * All matrices of one call run together, in three launches, or in
- * one where each has a side of at most 64 and the other of at most 704.  1 <= rows, cols <=
- * 65536, rows * cols <= 2^30, at most PF16_ORTHO_MAX_MATRICES matrices
+ * All matrices of one call run together, in three launches, or in one where
+ * each has a side of at most 64 and the other of at most 704.  1 <= rows,
+ * cols <= 65536, rows * cols <= 2^30 (PF16_ERR_SHAPE); at most
+ * PF16_ORTHO_MAX_MATRICES matrices and 2^38 bytes of workspace
  * (PF16_ERR_UNSUPPORTED beyond), 1 <= steps <= 16 (PF16_ERR_ARG).  The list
  * is host memory, read before the call returns.  Arrays are dense, row-major,
  * 16-byte aligned, and so is the workspace.  count may be 0 (nothing is
@@ -434,7 +439,9 @@ int pf16_orthogonalize(const pf16_ortho_matrix* mats, int32_t count, int32_t ste
  *   v = rn(momentum*v + g)
  *   u = g + momentum*v  with PF16_MUON_NESTEROV, else v   (v as stored)
  *   w = rn(w - lr*(scale*O(u) + wd*w)),  O(u) the result above, unrounded
- * with everything between the stored tensors in FP32.  lr, momentum and wd
+ * with everything between the stored tensors in FP32, but for the products'
+ * binary16 operands: one copy of each in all steps here (1.2e-3 to 1.8e-3 of
+ * O's norm), two where rows or cols <= 64.  lr, momentum and wd
  * are finite floats, scale too (per matrix: often sqrt(max(1, rows/cols)))
  * (PF16_ERR_ARG).  w and v overlap nothing else of the call (PF16_ERR_ARG). */
 #define PF16_MUON_NESTEROV 0x1u

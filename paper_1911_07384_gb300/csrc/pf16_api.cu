@@ -1667,7 +1667,7 @@ static int ortho_parts(long long numel) {
 }
 
 // Fills p's lists and returns the bytes of workspace (base may be null).
-static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t* base) {
+static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, bool muon, uint8_t* base) {
   int order[kOrthoMax];
   for (int i = 0; i < count; ++i) order[i] = i;
   std::sort(order, order + count, [&](int a, int b) {
@@ -1695,7 +1695,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     m.part0 = (int)parts;
     m.parts = ortho_parts((long long)s.rows * s.cols);
     parts += m.parts;
-    m.precise = m.mb <= kOrthoPrecise;
+    m.precise = !muon || m.mb <= kOrthoPrecise;
   }
   for (int i = 0; i < count; ++i) {
     OrthoMat& m = p->mat[i];
@@ -1705,8 +1705,6 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     // decides the order of the sum, which the other matrices of a call must not.
     const long long share = std::max(16ll, (long long)ortho_sym(ortho_tiles(m.mb)) * terms / kOrthoPairs);
     m.splits = (int)std::min<long long>(8, std::max<long long>(1, terms / share));
-    m.kper = cdiv(terms, m.splits);
-    m.splits = cdiv(terms, m.kper);
     const int mt = ortho_tiles(m.mb), tri = ortho_sym(mt);
     p->pre_pack[i] = (int)pack;
     p->pre_gram[i] = (int)gram;
@@ -1718,10 +1716,10 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, uint8_t
     sym += tri;
     wide += (long long)mt * cdiv(m.nb, 4);
   }
-  // The full product's tiles are 256 columns wide, or 128 where there are so few that the time of one
-  // counts, most of it its epilogue's, which reads and writes X (256, 128 wide: 512 x 512 200, 178 us;
-  // 256 x 2304 232, 201; 1000 x 2048, 32 tiles of 256, 249, 257).
-  p->full_blocks = wide >= kOrthoPairs / 4 ? 4 : 2;
+  // The full product's tiles are 256 columns wide, or 128 while every tile still has a pair of SMs for itself:
+  // one's time counts then, its product's and its epilogue's, which reads and writes X (256, 128 wide, pairs
+  // of copies: 1000 x 2048, 32 tiles of 256, 384, 358 us; single copies: there 249, 257, 512 x 512 200, 178).
+  p->full_blocks = wide > kOrthoPairs / 2 ? 4 : 2;
   for (int i = 0; i < count; ++i) {
     p->pre_full[i] = (int)full;
     full += (long long)ortho_tiles(p->mat[i].mb) * cdiv(p->mat[i].nb, p->full_blocks);
@@ -1799,7 +1797,8 @@ static size_t ortho_ws(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, in
   OrthoEntry e[kOrthoMax];
   if (ortho_entries(o, u, count, e) != PF16_OK || count == 0) return 0;
   OrthoParams p;
-  return ortho_plan(&p, e, count, nullptr);
+  const size_t need = ortho_plan(&p, e, count, u != nullptr, nullptr);
+  return need <= kOrthoMaxBytes ? need : 0;
 }
 
 static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int32_t count, int32_t steps, float lr,
@@ -1813,10 +1812,15 @@ static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int3
     if (!std::isfinite(e[i].scale)) return PF16_ERR_ARG;
   if (count == 0) return PF16_OK;
   OrthoParams p;
-  const size_t need = ortho_plan(&p, e, count, static_cast<uint8_t*>(ws));
+  const size_t need = ortho_plan(&p, e, count, u != nullptr, static_cast<uint8_t*>(ws));
+  if (need > kOrthoMaxBytes) return PF16_ERR_UNSUPPORTED;
   rc = ortho_pointers(e, count, u != nullptr, ws, ws_bytes, need);
   if (rc != PF16_OK) return rc;
   p.steps = steps;
+  for (int i = 0; i < count; ++i) {
+    OrthoMat& m = p.mat[i];
+    m.pairs_from = !m.precise ? steps : m.mb <= kOrthoPrecise ? 0 : std::max(0, steps - kOrthoPairSteps);
+  }
   p.muon = u != nullptr;
   p.nesterov = nesterov;
   p.lr = lr;

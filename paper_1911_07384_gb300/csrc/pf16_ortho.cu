@@ -97,8 +97,9 @@ __device__ __forceinline__ uint32_t low2(float x, float y, uint32_t h) {
   const float2 f = h22f(h);
   return f2h2(x - f.x, y - f.y);
 }
-// blocks in the sum over n of them: with two copies of the operands, three times as many
-__device__ __forceinline__ int ortho_sum(int n, int precise) { return precise ? 3 * n : n; }
+// whether a step multiplies pairs of binary16 copies, and the blocks in its sum over n: three times as many then
+__device__ __forceinline__ bool ortho_pairs(const OrthoMat& M, int step) { return step >= M.pairs_from; }
+__device__ __forceinline__ int ortho_sum(const OrthoMat& M, int step, int n) { return ortho_pairs(M, step) ? 3 * n : n; }
 
 // the largest i with pre[i] <= t, pre[0] = 0 and t < pre[n]
 __device__ __forceinline__ int find_mat(const int* pre, int n, int t) {
@@ -144,8 +145,9 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     const int local = (int)t - p.pre_gram[it.mat];
     it.split = local % M.splits;
     sym_tile(local / M.splits, it.I, it.J);
-    it.k0 = it.split * M.kper;
-    it.k1 = min(it.k0 + M.kper, ortho_sum(M.nb, M.precise));
+    const int terms = ortho_sum(M, it.step, M.nb);  // (at least as many as parts)
+    it.k0 = it.split * terms / M.splits;
+    it.k1 = (it.split + 1) * terms / M.splits;
   } else if (t < (uint32_t)(tg + ta)) {
     t -= (uint32_t)tg;
     it.kind = kSum;
@@ -159,7 +161,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     it.kind = kSym;
     it.mat = find_mat(p.pre_sym, n, (int)t);
     sym_tile((int)t - p.pre_sym[it.mat], it.I, it.J);
-    it.k1 = ortho_sum(p.mat[it.mat].mb, p.mat[it.mat].precise);
+    it.k1 = ortho_sum(p.mat[it.mat], it.step, p.mat[it.mat].mb);
   } else {
     t -= (uint32_t)(tg + ta + ts);
     it.kind = kFull;
@@ -168,7 +170,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     const int mt = ortho_tiles(p.mat[it.mat].mb);
     it.I = local % mt;  // column by column: neighbours share X's blocks
     it.J = local / mt;
-    it.k1 = ortho_sum(p.mat[it.mat].mb, p.mat[it.mat].precise);
+    it.k1 = ortho_sum(p.mat[it.mat], it.step, p.mat[it.mat].mb);
   }
   const OrthoMat& M = p.mat[it.mat];
   const int mt = ortho_tiles(M.mb), nt = (M.nb + p.full_blocks - 1) / p.full_blocks;
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(256) k_ortho_pack(const __grid_constant__ Orth
     v.y = f2h2(s[2] * kSx, s[3] * kSx);
     v.z = f2h2(s[4] * kSx, s[5] * kSx);
     v.w = f2h2(s[6] * kSx, s[7] * kSx);
-    if (M.precise) {
+    if (ortho_pairs(M, 0)) {
       const uint32_t h[4] = {v.x, v.y, v.z, v.w};
       uint32_t lo[4];
 #pragma unroll
@@ -453,7 +455,7 @@ struct Run {
 };
 // Whether one operand tile serves as both: on the diagonal, of single copies.
 __device__ __forceinline__ bool same_operand(const Item& it, const OrthoMat& M) {
-  return it.kind != kFull && it.I == it.J && !M.precise;
+  return it.kind != kFull && it.I == it.J && !ortho_pairs(M, it.step);
 }
 
 // One 8 KB block of the workspace, which `map` describes as rows of 128 bytes, signalling the leading
@@ -865,7 +867,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         : it.kind == kSym ? kC * kSb / (kSa * kSa)
                                           : 1.f / (kSx * kSb);
       const TileOut o{p, M, it, out, a16, x32, mul, stage_w, chunks, rr, lane, row, bj0, full_kind, final_step,
-                      M.precise ? L.lo : 0};
+                      ortho_pairs(M, it.step + full_kind) ? L.lo : 0};
       // FP32 parts of a split sum: this warp's rows and columns, four columns a lane at a time
       float4* part = reinterpret_cast<float4*>(
                          M.ws + L.part +
@@ -898,7 +900,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const int p0 = (((g & 3) * 2) ^ (rr & 7)) << 4, p1 = (((g & 3) * 2 + 1) ^ (rr & 7)) << 4;
           __stcg(reinterpret_cast<uint4*>(dst + p0), make_uint4(h[0], h[1], h[2], h[3]));
           __stcg(reinterpret_cast<uint4*>(dst + p1), make_uint4(h[4], h[5], h[6], h[7]));
-          if (M.precise) {
+          if (o.lo) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = low2(x[2 * j], x[2 * j + 1], h[j]);
             __stcg(reinterpret_cast<uint4*>(dst + L.lo + p0), make_uint4(h[0], h[1], h[2], h[3]));

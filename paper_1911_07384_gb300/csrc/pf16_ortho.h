@@ -9,6 +9,7 @@ namespace pf16 {
 constexpr int kOrthoMax = 256;       // matrices in one call (PF16_ORTHO_MAX_MATRICES)
 constexpr int kOrthoMaxParts = 512;  // partial sums of squares of one matrix
 constexpr int kOrthoBlk = 8192;      // bytes of a 64 x 64 binary16 block
+constexpr size_t kOrthoMaxBytes = (size_t)1 << 38;  // of a workspace: its rows of 128 bytes are counted by an int
 
 // One matrix.  Inside, it is m x n with m <= n (transposed when `tall`), kept as
 // a grid of mb x nb blocks of 64 x 64 elements, zero past its edges.  Binary16 blocks of two
@@ -24,8 +25,9 @@ struct OrthoMat {
   int mb, nb;
   int part0, parts;   // its partial sums of squares
   int tall;
-  int precise;        // operands as pairs of binary16 (kOrthoPrecise): sums three times as long
-  int splits, kper;   // X X^T: parts of its sum, and blocks in each
+  int precise;        // operands as pairs of binary16 copies, in steps from pairs_from on (kOrthoPairSteps)
+  int pairs_from;
+  int splits;         // X X^T: parts of its sum
   float scale;        // of the orthogonalised update in the weights' step
 };
 
@@ -63,10 +65,19 @@ __host__ __device__ inline int ortho_sym(int tiles) { return tiles * (tiles + 1)
 constexpr int kOrthoPart = 16384;
 constexpr int kOrthoSumItems = 8;
 
-// Matrices of at most one block of rows keep their operands as the sum of two binary16 copies, the
-// second of what the first's rounding left, and multiply high by high, high by low and low by high.
-// The roundings of single copies average out over many singular values; a few singular values can each
-// be several tenths of a percent off, and the products of so small a matrix cost nothing.
+// Operands as the sum of two binary16 copies, the second of what the first's rounding left: the products are then
+// high by high, high by low and low by high, 22 bits of each operand for three times the work.
+//  - pf16_orthogonalize multiplies pairs in its last kOrthoPairSteps steps, so that the rounding of its result is
+//    the larger part of its error: 2.1e-4 of the norm against 1.2e-3 to 1.8e-3 with single copies throughout
+//    (1000 x 2048: 249 us single, 317 two steps, 358 three, 405 all five; 4096 x 4096: 1046, 1659, 1984, 2639).
+//    A product's rounding weighs as b s^2 + c s^4 does, and by the third step from the end few singular values
+//    are large: what the steps before add is 1e-5 for a matrix of full rank, up to 9e-4 for one of rank 1.
+//  - The optimiser step multiplies single copies: its result is a fraction lr of a weight that is rounded to
+//    binary16 itself.
+//  - Matrices of at most kOrthoPrecise blocks of rows take pairs in every step of either call.  The roundings of
+//    single copies average out over many singular values; a few singular values can each be several tenths of a
+//    percent off, and the products of so small a matrix cost nothing.
+constexpr int kOrthoPairSteps = 3;
 constexpr int kOrthoPrecise = 1;
 
 // A call whose matrices all have at most kOrthoPrecise blocks of rows and kSmallBlocks of columns runs in one

@@ -10,37 +10,47 @@ def f16(x):
     return np.asarray(x, np.float64).astype(np.float16).astype(np.float64)
 
 
-def orthogonal(u, steps=5, copies=False):
-    """The definition; with copies, the products' operands rounded as the library states (X itself
-    is not): to binary16 in its scales, or, of matrices of at most 64 rows or columns, to two of them."""
+def orthogonal(u, steps=5, copies=0):
+    """The definition; with copies, the products' operands rounded as the library states (X itself is
+    not): to binary16 in its scales, or, in all but the first `copies - 1` steps and throughout where
+    the matrix has at most 64 rows or columns, to the sum of two such numbers."""
     a, b, c = COEFFS
     u = np.asarray(u, np.float64)
     size = np.sqrt((u * u).sum())
     if size == 0:
         return u
     x = (u.T if u.shape[0] > u.shape[1] else u) / size
-    if copies and x.shape[0] <= 64:  # two copies: what the second leaves
-        r = lambda v, s: (f16(v * s) + f16(v * s - f16(v * s))) / s
-    else:
-        r = (lambda v, s: f16(v * s) / s) if copies else (lambda v, s: v)
-    for _ in range(steps):
+    for i in range(steps):
+        if not copies:
+            r = lambda v, s: v
+        elif i < copies - 1 and x.shape[0] > 64:
+            r = lambda v, s: f16(v * s) / s
+        else:
+            r = lambda v, s: (f16(v * s) + f16(v * s - f16(v * s))) / s
         h = r(x, 2.0 ** 15)
         s = r(h @ h.T, 2.0 ** 15)
         x = a * x + r(b * s + c * (s @ s), 2.0 ** 14) @ h
     return x.T if u.shape[0] > u.shape[1] else x
 
 
-def orthogonal_tolerance(u, steps=5):
-    """How far (Frobenius norm) the library's FP32 result may be from the exact one.
+def orthogonal_tolerance(u, steps=5, single=5):
+    """How far (Frobenius norm) the library's FP32 result may be from the exact one, when its first
+    `single` steps multiply single copies.
 
     Its error is that of the stated roundings of the operands, whose size the emulation
     gives.  Another summation order draws other roundings of the same size: the norms of
     two such draws over n independent elements differ by a few times n^-1/2 of themselves,
     and a matrix of a few elements can have one draw near zero, so three times the
     emulation's error, and one half step (2^-11) per product chain of the result for the
-    draws that come out near zero.  FP32 sums add less than 2^-20."""
+    draws that come out near zero.  Where the last step multiplies pairs, the emulation has 2^-22 of
+    each operand; FP32 sums of 3 n / 16 instructions' products are up to 2^-24 of their
+    magnitudes off at each, twice in B and once in X, and a step passes an error on at most 3.44 times
+    as large: 2^-24 (3 n / 16) times 16 covers the last three, beside 2^-12 for the steps before them."""
     e = orthogonal(u, steps)
-    return 3 * np.linalg.norm(orthogonal(u, steps, copies=True) - e) + 2 * U16 * np.linalg.norm(e)
+    off = np.linalg.norm(orthogonal(u, steps, copies=single + 1) - e)
+    if single < steps or min(u.shape) <= 64:
+        return 3 * off + (U16 / 2 + 3 * max(u.shape) * 2.0 ** -24) * np.linalg.norm(e)
+    return 3 * off + 2 * U16 * np.linalg.norm(e)
 
 
 def muon(w, v, g, lr, momentum, wd, scale, nesterov, steps=5):

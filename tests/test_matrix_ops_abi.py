@@ -65,6 +65,11 @@ def test_list_lengths():
     many = pf16.ortho_list([(T(G.at + 256 * i), T(O.at + 256 * i), 4, 4) for i in range(257)])
     assert pf16.ortho_workspace_size(many) == 0
     refused(pf16.PF16_ERR_UNSUPPORTED, pf16.orthogonalize, many, T(WS.at, MIB))
+    G30 = 1 << 30  # more than 2^38 bytes of workspace
+    vast = pf16.ortho_list([(T(4 * G30 * (i + 1)), T(4 * G30 * (i + 65)), 32768, 32768) for i in range(64)])
+    assert pf16.ortho_workspace_size(vast) == 0
+    refused(pf16.PF16_ERR_UNSUPPORTED, pf16.orthogonalize, vast, T(4 * G30 * 200, 1 << 39))
+    assert pf16.ortho_workspace_size((pf16.OrthoMatrix * 8).from_buffer(vast)) > 8 * G30 * 8
     full = (pf16.OrthoMatrix * 256).from_buffer(many)
     assert pf16.ortho_workspace_size(full) > 0
     pf16.orthogonalize(pf16.ortho_list([]), None, stream=0)  # nothing to do
@@ -96,16 +101,17 @@ def test_muon_refusals():
 
 def test_workspace_covers_the_padded_matrices():
     """X twice in binary16 and once in FP32, S and the quintic's factor, in blocks of 64 x 64, the
-    binary16 ones for even numbers of blocks, and twice for matrices of one block of rows; and FP32 parts
-    of S where its sums are split, at most eight of them."""
+    binary16 ones for even numbers of blocks, and twice where products take pairs of them (not in the
+    optimiser's step of more than one block of rows); and FP32 parts of S where its sums are split, at
+    most eight of them."""
     for rows, cols in ((1, 1), (64, 64), (65, 64), (1000, 2048), (2048, 1000), (512, 4608)):
         m, n = (-(-s // 64) * 64 for s in sorted((rows, cols)))
         m2, n2 = (-(-s // 128) * 128 for s in (m, n))
-        need = pf16.ortho_workspace_size(pf16.ortho_list([(G, O, rows, cols)]))
         parts = 8 * 4 * (-(-m // 256) * 256) ** 2
-        copies = 2 if m == 64 else 1
-        assert 0 <= need - (copies * (4 * m2 * n2 + 4 * m2 * m2) + 4 * m * n) <= parts + 4096
-        assert need == pf16.muon_workspace_size(pf16.muon_list([(O, V, G, rows, cols, 1.0)]))
+        for copies, need in ((2, pf16.ortho_workspace_size(pf16.ortho_list([(G, O, rows, cols)]))),
+                             (2 if m == 64 else 1,
+                              pf16.muon_workspace_size(pf16.muon_list([(O, V, G, rows, cols, 1.0)])))):
+            assert 0 <= need - (copies * (4 * m2 * n2 + 4 * m2 * m2) + 4 * m * n) <= parts + 4096
 
 
 def test_quantize_refusals():
