@@ -1679,7 +1679,7 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, bool mu
   p->ticket = reinterpret_cast<uint32_t*>(base);
   p->done = p->ticket + 4;
   const size_t words = 4 + (size_t)count;
-  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0, wide = 0;
+  long long parts = 0, pack = 0, gram = 0, sum = 0, sym = 0, full = 0, wide = 0, products = 0;
   for (int i = 0; i < count; ++i) {
     const OrthoEntry& s = e[order[i]];
     OrthoMat& m = p->mat[i];
@@ -1696,14 +1696,16 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, bool mu
     m.parts = ortho_parts((long long)s.rows * s.cols);
     parts += m.parts;
     m.precise = !muon || m.mb <= kOrthoPrecise;
+    products += (long long)ortho_sym(ortho_tiles(m.mb)) * (m.precise ? 3 * m.nb : m.nb);
   }
   for (int i = 0; i < count; ++i) {
     OrthoMat& m = p->mat[i];
     const int terms = m.precise ? 3 * m.nb : m.nb;
-    // X X^T's sum split so that the matrix would keep every pair of SMs busy, but into no less than 16 blocks
-    // (about 4 us; the parts' store, their phase and its wait take about 8).  By its own size alone: the split
-    // decides the order of the sum, which the other matrices of a call must not.
-    const long long share = std::max(16ll, (long long)ortho_sym(ortho_tiles(m.mb)) * terms / kOrthoPairs);
+    // X X^T's sum split so that no item is longer than a pair of SMs' share of all matrices' such products, but
+    // into no less than 16 blocks (about 4 us; the parts' store, their phase and its wait take about 8).  Three
+    // matrices of 512 x 4608 in a call take 303 us, with whole sums 330; 256 x 2304 248, 307; all filters of a
+    // ResNet-50 646, whole 630, at its own share, whatever the others', 695; with pairs of copies 742, 778, 890.
+    const long long share = std::max(16ll, products / kOrthoPairs);
     m.splits = (int)std::min<long long>(8, std::max<long long>(1, terms / share));
     const int mt = ortho_tiles(m.mb), tri = ortho_sym(mt);
     p->pre_pack[i] = (int)pack;

@@ -69,7 +69,8 @@ constexpr int kOrthoSumItems = 8;
 // high by high, high by low and low by high, 22 bits of each operand for three times the work.
 //  - pf16_orthogonalize multiplies pairs in its last kOrthoPairSteps steps, so that the rounding of its result is
 //    the larger part of its error: 2.1e-4 of the norm against 1.2e-3 to 1.8e-3 with single copies throughout
-//    (1000 x 2048: 249 us single, 317 two steps, 358 three, 405 all five; 4096 x 4096: 1046, 1659, 1984, 2639).
+//    (1000 x 2048, tiles 256 wide: 249 us single, 345 two steps, 384 three, 438 all five; 4096 x 4096: 1046, 1659,
+//    1984, 2639; two steps leave 3.7e-4).
 //    A product's rounding weighs as b s^2 + c s^4 does, and by the third step from the end few singular values
 //    are large: what the steps before add is 1e-5 for a matrix of full rank, up to 9e-4 for one of rank 1.
 //  - The optimiser step multiplies single copies: its result is a fraction lr of a weight that is rounded to
