@@ -53,8 +53,10 @@ __device__ __forceinline__ float stored_scale(float a) {
 }  // namespace
 
 // R rows by each group of G threads (G <= 32: part of a warp; 256: the CTA).
-// VEC: rows of whole 16-byte vectors, of which a thread keeps its first KEEP in registers between the
-// maximum and the rounding and reads the others twice.
+// Vectors of 8 values at multiples of 8 in the whole array, for which x's 16 bytes and q's 8 are aligned; unless VEC
+// (k a multiple of 8) a row's first and last are shared with its neighbours: their values count as zeros, and the
+// row's own integers are stored one at a time.  A thread keeps its first KEEP vectors in registers between
+// the maximum and the rounding and reads the others twice.
 // Bound by memory: every load of a thread's rows is issued before the first maximum is taken.
 template <int G, int KEEP, int R, bool VEC>
 __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict__ x, int8_t* __restrict__ q,
@@ -63,34 +65,53 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
   constexpr int GROUPS = 256 / G;
   const int g = (int)threadIdx.x % G;
   const long long row0 = (long long)blockIdx.x * (GROUPS * R) + threadIdx.x / G;  // and every GROUPS-th from there
-  const int nv = k >> 3;
-  uint4 keep[R][KEEP > 0 ? KEEP : 1];
-  uint32_t mx[R];
-  if (VEC) {
+  // a row's first element in its first vector, and its vectors
+  auto lead = [&](long long row) { return VEC ? 0 : (int)((unsigned)(row * k) & 7u); };
+  auto vectors = [&](long long row) { return (lead(row) + k + 7) >> 3; };
+  auto load = [&](long long row, int c) {
+    const int first = lead(row);
+    const long long at = row * k - first + 8ll * c;
+    uint4 v;
+    if (VEC || at + 8 <= m * k) {
+      v = __ldcs(reinterpret_cast<const uint4*>(x + at));
+    } else {  // the array's last
+      uint32_t h[4];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const long long row = row0 + r * GROUPS;
-      const uint4* xv = reinterpret_cast<const uint4*>(x + (row < m ? row : 0) * k);
-#pragma unroll
-      for (int i = 0; i < KEEP; ++i)
-        keep[r][i] = row < m && g + i * G < nv ? __ldcs(xv + g + i * G) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < 4; ++j)
+        h[j] = (at + 2 * j < m * k ? (uint32_t)x[at + 2 * j] : 0u) |
+               (at + 2 * j + 1 < m * k ? (uint32_t)x[at + 2 * j + 1] << 16 : 0u);
+      v = make_uint4(h[0], h[1], h[2], h[3]);
     }
+    if (!VEC) {
+      const int i = 8 * c - first;  // of the row
+      if (i < 0 || i + 8 > k) {
+        auto own = [&](uint32_t h, int j) {
+          return (i + j >= 0 && i + j < k ? h & 0xffffu : 0u) | (i + j + 1 >= 0 && i + j + 1 < k ? h & 0xffff0000u : 0u);
+        };
+        v = make_uint4(own(v.x, 0), own(v.y, 2), own(v.z, 4), own(v.w, 6));
+      }
+    }
+    return v;
+  };
+  uint4 keep[R][KEEP];
+  uint32_t mx[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const long long row = row0 + r * GROUPS;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+      keep[r][i] = row < m && g + i * G < vectors(row) ? load(row, g + i * G) : make_uint4(0, 0, 0, 0);
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const long long row = row0 + r * GROUPS;
-    const uint16_t* xr = x + (row < m ? row : 0) * k;
     uint32_t v = 0;
-    if (VEC) {
 #pragma unroll
-      for (int i = 0; i < KEEP; ++i)
-        v = abs_max2(abs_max2(abs_max2(abs_max2(v, keep[r][i].x), keep[r][i].y), keep[r][i].z), keep[r][i].w);
-      for (int c = g + KEEP * G; c < (row < m ? nv : 0); c += G) {
-        const uint4 u = reinterpret_cast<const uint4*>(xr)[c];
-        v = abs_max2(abs_max2(abs_max2(abs_max2(v, u.x), u.y), u.z), u.w);
-      }
-    } else {
-      for (int c = g; c < (row < m ? k : 0); c += G) v = abs_max2(v, (uint32_t)xr[c]);
+    for (int i = 0; i < KEEP; ++i)
+      v = abs_max2(abs_max2(abs_max2(abs_max2(v, keep[r][i].x), keep[r][i].y), keep[r][i].z), keep[r][i].w);
+    for (int c = g + KEEP * G; c < (row < m ? vectors(row) : 0); c += G) {
+      const uint4 u = load(row, c);
+      v = abs_max2(abs_max2(abs_max2(abs_max2(v, u.x), u.y), u.z), u.w);
     }
     mx[r] = v;
   }
@@ -116,36 +137,38 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
   for (int r = 0; r < R; ++r) {
     const long long row = row0 + r * GROUPS;
     if (row >= m) break;
-    const uint16_t* xr = x + row * k;
     const float a = h2f((uint16_t)mx[r]);
     const RowScale s = row_scale(a);
     if (g == 0) scale[row] = stored_scale(a);
-    int8_t* qr = q + row * k;
     // with r = 0 (a zero row, or one that is not finite) the integers are zero
-    if (VEC) {
-      const uint4* xv = reinterpret_cast<const uint4*>(xr);
-      auto put = [&](int c, const uint4& v) {
-        const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-        uint2 o = make_uint2(0, 0);
-        if (s.r != 0.f) {
-          uint32_t b[8];
+    auto put = [&](int c, const uint4& v) {
+      const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+      uint2 o = make_uint2(0, 0);
+      if (s.r != 0.f) {
+        uint32_t b[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            b[2 * j] = quant1((uint16_t)h[j], s);
-            b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
-          }
-          o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
-          o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
+        for (int j = 0; j < 4; ++j) {
+          b[2 * j] = quant1((uint16_t)h[j], s);
+          b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
         }
-        __stcs(reinterpret_cast<uint2*>(qr) + c, o);
-      };
+        o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
+        o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
+      }
+      const int i = 8 * c - lead(row);
+      int8_t* at = q + row * k + i;
+      if (VEC || (i >= 0 && i + 8 <= k)) {
+        __stcs(reinterpret_cast<uint2*>(at), o);
+      } else {
 #pragma unroll
-      for (int i = 0; i < KEEP; ++i)
-        if (g + i * G < nv) put(g + i * G, keep[r][i]);
-      for (int c = g + KEEP * G; c < nv; c += G) put(c, xv[c]);
-    } else {
-      for (int c = g; c < k; c += G) qr[c] = s.r != 0.f ? (int8_t)quant1(xr[c], s) : (int8_t)0;
-    }
+        for (int j = 0; j < 8; ++j)
+          if (i + j >= 0 && i + j < k) at[j] = (int8_t)((j < 4 ? o.x : o.y) >> ((j & 3) * 8));
+      }
+    };
+    const int nv = vectors(row);
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+      if (g + i * G < nv) put(g + i * G, keep[r][i]);
+    for (int c = g + KEEP * G; c < nv; c += G) put(c, load(row, c));
   }
 }
 
@@ -155,20 +178,23 @@ static cudaError_t quantize_g(const uint16_t* x, int8_t* q, float* scale, long l
   const dim3 grid((unsigned)((m + rows - 1) / rows)), block(256);
   const cudaError_t e = (k & 7) == 0
                             ? launch_pdl(k_quantize_i8<G, KEEP, R, true>, grid, block, 0, s, x, q, scale, m, k)
-                            : launch_pdl(k_quantize_i8<G, 0, R, false>, grid, block, 0, s, x, q, scale, m, k);
+                            : launch_pdl(k_quantize_i8<G, KEEP, R, false>, grid, block, 0, s, x, q, scale, m, k);
   return e == cudaSuccess ? counted_launches(1) : e;
 }
 
 cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s) {
   // Few lanes a row and four vectors a lane: what a row costs apart from its elements (its reduction and two
-  // divisions, by all its lanes) took longer than memory with a warp a row (802816 x 256: 130 us).
-  if (k <= 64) return quantize_g<2, 4, 1>(x, q, scale, m, k, s);
-  if (k <= 128) return quantize_g<4, 4, 1>(x, q, scale, m, k, s);
-  if (k <= 256) return quantize_g<8, 4, 1>(x, q, scale, m, k, s);
-  if (k <= 512) return quantize_g<16, 4, 1>(x, q, scale, m, k, s);
-  if (k <= 1024) return quantize_g<32, 4, 1>(x, q, scale, m, k, s);
-  if (k <= 2048) return m < 2048 ? quantize_g<256, 1, 1>(x, q, scale, m, k, s) : quantize_g<256, 1, 4>(x, q, scale, m, k, s);
-  if (k <= 4096) return quantize_g<256, 2, 1>(x, q, scale, m, k, s);
+  // divisions, by all its lanes) took longer than memory with a warp a row (802816 x 256: 130 us, 89 with eight lanes).  A CTA a row from 2049
+  // values on, and for few rows: 2000 x 2048 4.2 us by warps, 4.2 by CTAs; 12544 x 2048 13.9, 18.7 (four rows a CTA);
+  // 4096 x 4096 11.4, 10.6.
+  const int n = (k & 7) == 0 ? k : (k + 14) / 8 * 8;  // values in a row's vectors, at most
+  if (n <= 64) return quantize_g<2, 4, 1>(x, q, scale, m, k, s);
+  if (n <= 128) return quantize_g<4, 4, 1>(x, q, scale, m, k, s);
+  if (n <= 256) return quantize_g<8, 4, 1>(x, q, scale, m, k, s);
+  if (n <= 512) return quantize_g<16, 4, 1>(x, q, scale, m, k, s);
+  if (n <= 1024) return quantize_g<32, 4, 1>(x, q, scale, m, k, s);
+  if (n <= 2048) return m < 2048 ? quantize_g<256, 1, 1>(x, q, scale, m, k, s) : quantize_g<32, 8, 1>(x, q, scale, m, k, s);
+  if (n <= 4096) return quantize_g<256, 2, 1>(x, q, scale, m, k, s);
   return quantize_g<256, 8, 1>(x, q, scale, m, k, s);
 }
 
@@ -189,10 +215,25 @@ __device__ __forceinline__ uint4 ld_once(const uint4* p) {
   return v;
 }
 
-// 16 bytes of a row of k bytes from byte c on, zero past its end; ALIGNED: rows start at multiples
-// of 16 and hold whole vectors.
+// 16 bytes from p on, at any address, of an array whose aligned 16 bytes before and after them are its own.  No
+// branch: a thread's loads are all issued before the first is shifted into place.
+__device__ __forceinline__ uint4 load16_inside(const int8_t* p) {
+  const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
+  const uint4* q = reinterpret_cast<const uint4*>(p - lead);
+  const uint4 a = __ldg(q), b = __ldg(q + 1);
+  const bool two = lead & 8, one = lead & 4;
+  const uint32_t v0 = two ? a.z : a.x, v1 = two ? a.w : a.y, v2 = two ? b.x : a.z, v3 = two ? b.y : a.w,
+                 v4 = two ? b.z : b.x, v5 = two ? b.w : b.y;
+  const uint32_t w0 = one ? v1 : v0, w1 = one ? v2 : v1, w2 = one ? v3 : v2, w3 = one ? v4 : v3, w4 = one ? v5 : v4;
+  const uint32_t s = (lead & 3) * 8;
+  return make_uint4(__funnelshift_r(w0, w1, s), __funnelshift_r(w1, w2, s), __funnelshift_r(w2, w3, s),
+                    __funnelshift_r(w3, w4, s));
+}
+
+// 16 bytes of a row of k bytes from byte c on, zero past its end, of an array that ends at `end`;
+// ALIGNED: rows start at multiples of 16 and hold whole vectors.
 template <bool ALIGNED, bool ONCE = false>
-__device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
+__device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k, const int8_t* end) {
   // (the pointer inside the guard: named before it, the load became a branch, and large products 10% slower)
   if (ALIGNED && ONCE) return c < k ? ld_once(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
   if (ALIGNED) return c < k ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
@@ -201,15 +242,17 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
     const uint2 z = make_uint2(0, 0), lo = c < k ? __ldg(p) : z, hi = c + 8 < k ? __ldg(p + 1) : z;
     return make_uint4(lo.x, lo.y, hi.x, hi.y);
   }
-  // Whole words around the 16 bytes while they end inside the row (they start in the
-  // array: rows before this one, or the array's aligned start, precede it).
-  const int lead = (int)(reinterpret_cast<uintptr_t>(row + c) & 3u);
-  if (c + 16 + ((4 - lead) & 3) <= k) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(row + c - lead);
-    const uint32_t w0 = __ldg(w), w1 = __ldg(w + 1), w2 = __ldg(w + 2), w3 = __ldg(w + 3);
-    const uint32_t w4 = lead ? __ldg(w + 4) : 0u;
-    return make_uint4(__funnelshift_r(w0, w1, lead * 8), __funnelshift_r(w1, w2, lead * 8),
-                      __funnelshift_r(w2, w3, lead * 8), __funnelshift_r(w3, w4, lead * 8));
+  if (c >= k) return make_uint4(0, 0, 0, 0);
+  if (end - row >= c + 32) {  // into the rows behind this one, but not past the array
+    uint4 v = load16_inside(row + c);
+    if (c + 16 > k) {
+      const int n = (k - c) * 8;  // bits
+      auto cut = [n](uint32_t w, int from) {
+        return n >= from + 32 ? w : n <= from ? 0u : w & ((1u << (n - from)) - 1);
+      };
+      v = make_uint4(cut(v.x, 0), cut(v.y, 32), cut(v.z, 64), cut(v.w, 96));
+    }
+    return v;
   }
   uint32_t v[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -222,6 +265,7 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int c, int k) {
 
 template <bool ALIGNED>
 __global__ void __launch_bounds__(256, ALIGNED ? 8 : 5) k_linear_i8_rows(const LinearI8 a) {
+  const int8_t *const wend = a.w + (long long)a.n * a.k, *const xend = a.x + (long long)a.m * a.k;
   pdl_wait();
   const int lane = (int)threadIdx.x & 31;
   const int j = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), i = (int)blockIdx.y;
@@ -232,11 +276,17 @@ __global__ void __launch_bounds__(256, ALIGNED ? 8 : 5) k_linear_i8_rows(const L
 #pragma unroll 1
   for (int c = lane * 16; c < a.k; c += 2048) {
     uint4 wv[4];  // four loads of the weight in flight
+    const bool inside = !ALIGNED && (a.k & 7) && c - lane * 16 + 2064 <= a.k;  // all lanes' bytes and 16 more
+    if (inside) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) wv[u] = load16<ALIGNED, true>(w, c + u * 512, a.k);
+      for (int u = 0; u < 4; ++u) wv[u] = load16_inside(w + c + u * 512);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) wv[u] = load16<ALIGNED, true>(w, c + u * 512, a.k, wend);
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const uint4 xv = load16<ALIGNED>(x, c + u * 512, a.k);
+      const uint4 xv = inside ? load16_inside(x + c + u * 512) : load16<ALIGNED>(x, c + u * 512, a.k, xend);
       acc = __dp4a((int)wv[u].x, (int)xv.x, acc);
       acc = __dp4a((int)wv[u].y, (int)xv.y, acc);
       acc = __dp4a((int)wv[u].z, (int)xv.z, acc);
@@ -287,6 +337,7 @@ __device__ __forceinline__ void widen16(const uint4& v, uint32_t (&h)[8]) {
 template <int NT, int RT, bool ALIGNED>
 __global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
   __shared__ int part[8][RT * NT * 4][32];
+  const int8_t *const wend = a.w + (long long)a.n * a.k, *const xend = a.x + (long long)a.m * a.k;
   pdl_wait();
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const int j0 = (int)blockIdx.x * (16 * RT), g = lane >> 2, c0 = (lane & 3) * 16;
@@ -307,10 +358,19 @@ __global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
 #pragma unroll 1
   for (int c = warp * 128 + c0; c - c0 < a.k; c += DEEP * 512) {  // 128 bytes of a row by a warp, in two loads
     uint4 u[DEEP][2 * RT];
+    // (a warp's chunks end 144 past the start of its last pair of them)
+    if (!ALIGNED && (a.k & 7) && c - c0 + (DEEP / 2 - 1) * 1024 + 144 <= a.k) {
 #pragma unroll
-    for (int d = 0; d < DEEP; ++d)
+      for (int d = 0; d < DEEP; ++d)
 #pragma unroll
-      for (int r = 0; r < 2 * RT; ++r) u[d][r] = load16<ALIGNED, true>(w[r], c + (d >> 1) * 1024 + (d & 1) * 64, a.k);
+        for (int r = 0; r < 2 * RT; ++r) u[d][r] = load16_inside(w[r] + c + (d >> 1) * 1024 + (d & 1) * 64);
+    } else {
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+        for (int r = 0; r < 2 * RT; ++r)
+          u[d][r] = load16<ALIGNED, true>(w[r], c + (d >> 1) * 1024 + (d & 1) * 64, a.k, wend);
+    }
 #pragma unroll
     for (int d = 0; d < DEEP; ++d) {
       uint32_t h[2 * RT][8];
@@ -320,7 +380,7 @@ __global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
       for (int t = 0; t < NT; ++t) {
         const int i = t * 8 + g;
         uint32_t b[8];
-        widen16(i < a.m ? load16<ALIGNED>(a.x + (long long)i * a.k, c + (d >> 1) * 1024 + (d & 1) * 64, a.k)
+        widen16(i < a.m ? load16<ALIGNED>(a.x + (long long)i * a.k, c + (d >> 1) * 1024 + (d & 1) * 64, a.k, xend)
                          : make_uint4(0, 0, 0, 0),
                 b);
 #pragma unroll
@@ -416,11 +476,20 @@ struct Feed {
     pb = p + (pl > 0 ? (long long)(p0 + row) * k : 0);
     qb = q + (ql > 0 ? (long long)(q0 + row) * k : 0);
   }
+  // whether a stage's bytes of every row, and 16 more, lie inside the row
+  __device__ __forceinline__ bool inside(int stage) const { return !ALIGNED && (k & 7) && stage * 128 + 144 <= k; }
+  template <bool INSIDE = false>
   __device__ __forceinline__ void fetch(int u, int stage, uint4& dst) const {  // (u is a constant where this is expanded)
     const bool in_p = u < UP;
     const int i = in_p ? u : u - UP;
+    if (INSIDE) {  // rows past the end as the array's first: nobody stores what they are multiplied into
+      dst = load16_inside((i * 32 < (in_p ? pl : ql) ? (in_p ? pb : qb) + i * step : in_p ? p : q) + stage * 128 +
+                          (ct & 7) * 16);
+      return;
+    }
     dst = i * 32 < (in_p ? pl : ql)
-              ? load16<ALIGNED>((in_p ? pb : qb) + i * step, stage * 128 + (ct & 7) * 16, k)
+              ? load16<ALIGNED>((in_p ? pb : qb) + i * step, stage * 128 + (ct & 7) * 16, k,
+                                (in_p ? p + (long long)prows * k : q + (long long)qrows * k))
               : make_uint4(0, 0, 0, 0);
   }
   // a unit into the two K-blocks' tiles of a stage, HALF apart: P's 128 rows, then Q's
@@ -558,10 +627,18 @@ __global__ void __launch_bounds__(kI8Threads, I8Cfg<BN>::CTAS)
           atomicCAS(status, 0, -7);
           break;
         }
+        const int ahead = i + d + Cfg::DIST;
+        if (ahead < ns && feed.inside(s0 + ahead)) {
 #pragma unroll
-        for (int u = 0; u < Cfg::U; ++u) {
-          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
-          if (i + d + Cfg::DIST < ns) feed.fetch(u, s0 + i + d + Cfg::DIST, raw[d][u]);
+          for (int u = 0; u < Cfg::U; ++u) feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) feed.template fetch<true>(u, s0 + ahead, raw[d][u]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) {
+            feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+            if (ahead < ns) feed.fetch(u, s0 + ahead, raw[d][u]);
+          }
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -875,10 +952,17 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           atomicCAS(status, 0, -7);
           break;
         }
+        if (feed.inside(fs)) {
 #pragma unroll
-        for (int u = 0; u < Cfg::U; ++u) {
-          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
-          feed.fetch(u, fs, raw[d][u]);
+          for (int u = 0; u < Cfg::U; ++u) feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) feed.template fetch<true>(u, fs, raw[d][u]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) {
+            feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+            feed.fetch(u, fs, raw[d][u]);
+          }
         }
         next();
         fence_proxy_async_smem();
@@ -1069,10 +1153,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           atomicCAS(status, 0, -7);
           break;
         }
+        if (feed.inside(fs)) {
 #pragma unroll
-        for (int u = 0; u < Cfg::U; ++u) {
-          feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
-          feed.fetch(u, fs, raw[d][u]);
+          for (int u = 0; u < Cfg::U; ++u) feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) feed.template fetch<true>(u, fs, raw[d][u]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < Cfg::U; ++u) {
+            feed.template put<Cfg::HALF>(u, smem + stage * Cfg::STAGE, raw[d][u]);
+            feed.fetch(u, fs, raw[d][u]);
+          }
         }
         next();
         fence_proxy_async_smem();

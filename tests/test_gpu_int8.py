@@ -43,7 +43,8 @@ def test_quantize(m, k):
     check_quantize((rng.standard_normal((m, k)) * 2.0 ** rng.integers(-12, 10, (m, 1))).astype(np.float16))
 
 
-@pytest.mark.parametrize("m,k", [(2, 8192), (3, 8200), (2, 30000), (1, 65537), (70001, 8)])
+@pytest.mark.parametrize("m,k", [(2, 8192), (3, 8200), (2, 30000), (1, 65537), (70001, 8), (2500, 1065), (2100, 2047), (2050, 2048),
+                                  (30, 2041), (40001, 9), (5, 16385), (300, 1023), (9, 4089)])
 def test_quantize_long_and_many_rows(m, k):
     rng = np.random.default_rng(k)
     check_quantize(rng.standard_normal((m, k)).astype(np.float16))
@@ -127,6 +128,17 @@ def test_linear(m, n, k):
         x, sx, w, sw, b = operands(rng, m, n, k)
         b = b if bias else None
         check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 37, 4097), (5, 61, 2051), (8, 50, 4003), (16, 33, 2113), (16, 5000, 1301), (24, 300, 4001),
+                                   (32, 77, 1169), (60, 500, 1001), (64, 130, 2047), (130, 70, 1171), (1000, 1000, 1023),
+                                   (512, 4096, 1001), (2050, 2049, 1041), (300, 300, 145), (300, 300, 143), (3000, 900, 159)])
+def test_linear_rows_at_any_byte(m, n, k):
+    """Rows of every alignment, read 16 bytes at a time: what neighbours and the arrays' ends hold does not count."""
+    rng = np.random.default_rng(m + n + k)
+    x, sx, w, sw, b = operands(rng, m, n, k, extreme=True)
+    sx *= np.float32(2.0 ** -8)
+    check_linear(x, sx, w, sw, b, linear(x, sx, w, sw, b))
 
 
 # many tiles: every CTA or pair of them has several, the last ones ragged in all three sizes
