@@ -335,7 +335,7 @@ __device__ __forceinline__ void widen16(const uint4& v, uint32_t (&h)[8]) {
 }  // namespace
 
 template <int NT, int RT, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
+__global__ void __launch_bounds__(256, NT < 4 ? 2 : 1) k_linear_i8_few(const LinearI8 a) {
   __shared__ int part[8][RT * NT * 4][32];
   const int8_t *const wend = a.w + (long long)a.n * a.k, *const xend = a.x + (long long)a.m * a.k;
   pdl_wait();
@@ -355,9 +355,13 @@ __global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) acc[r][t][q] = 0.f;
   constexpr int DEEP = RT > 1 ? 2 : 4;  // chunks of a warp in flight
-#pragma unroll 1
-  for (int c = warp * 128 + c0; c - c0 < a.k; c += DEEP * 512) {  // 128 bytes of a row by a warp, in two loads
-    uint4 u[DEEP][2 * RT];
+  // The next chunks of the weights are loaded before these are multiplied, and the rows of x, in the wider variant,
+  // all at once (16 8192 8192: 18.1 us without, 16.0 with the first, 15.4 with both; 8 8192 8192, one group of
+  // rows: 14.7, 14.6, 15.5).  Not for 32 rows or rows at any byte, whose registers spill then (32 4096 1024
+  // 3.6, 3.85; 16 8001 4001 17.6, 20.0).
+  constexpr bool AHEAD = ALIGNED && NT < 4, TOGETHER = AHEAD && NT > 1 && RT > 1;
+  uint4 u[DEEP][2 * RT];
+  auto fetch = [&](int c) {  // 128 bytes of a row by a warp, in two loads
     // (a warp's chunks end 144 past the start of its last pair of them)
     if (!ALIGNED && (a.k & 7) && c - c0 + (DEEP / 2 - 1) * 1024 + 144 <= a.k) {
 #pragma unroll
@@ -371,17 +375,39 @@ __global__ void __launch_bounds__(256) k_linear_i8_few(const LinearI8 a) {
         for (int r = 0; r < 2 * RT; ++r)
           u[d][r] = load16<ALIGNED, true>(w[r], c + (d >> 1) * 1024 + (d & 1) * 64, a.k, wend);
     }
+  };
+  if (AHEAD) fetch(warp * 128 + c0);
+#pragma unroll 1
+  for (int c = warp * 128 + c0; c - c0 < a.k; c += DEEP * 512) {
+    if (!AHEAD) fetch(c);
+    uint4 now[DEEP][2 * RT];
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+      for (int r = 0; r < 2 * RT; ++r) now[d][r] = u[d][r];
+    uint4 xs[DEEP][TOGETHER ? NT : 1];
+    if (TOGETHER) {
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          xs[d][t] = t * 8 + g < a.m ? load16<ALIGNED>(a.x + (long long)(t * 8 + g) * a.k,
+                                                       c + (d >> 1) * 1024 + (d & 1) * 64, a.k, xend)
+                                     : make_uint4(0, 0, 0, 0);
+    }
+    if (AHEAD) fetch(c + DEEP * 512);
 #pragma unroll
     for (int d = 0; d < DEEP; ++d) {
       uint32_t h[2 * RT][8];
 #pragma unroll
-      for (int r = 0; r < 2 * RT; ++r) widen16(u[d][r], h[r]);
+      for (int r = 0; r < 2 * RT; ++r) widen16(now[d][r], h[r]);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int i = t * 8 + g;
         uint32_t b[8];
-        widen16(i < a.m ? load16<ALIGNED>(a.x + (long long)i * a.k, c + (d >> 1) * 1024 + (d & 1) * 64, a.k, xend)
-                         : make_uint4(0, 0, 0, 0),
+        widen16(TOGETHER  ? xs[d][t]
+                : i < a.m ? load16<ALIGNED>(a.x + (long long)i * a.k, c + (d >> 1) * 1024 + (d & 1) * 64, a.k, xend)
+                          : make_uint4(0, 0, 0, 0),
                 b);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -1289,15 +1315,15 @@ cudaError_t linear_few(const LinearI8& a, cudaStream_t s) {
 //
 // A warp an element: from HBM once, from the L2 for further rows (b = n k bytes):
 //   m n k          warps  mma.sync        m n k          warps  mma.sync
-//   2 1008 2048     2.1     2.6           2 8192 8192    15.9    15.3
-//   8 1008 2048     2.8     2.6           8 8192 8192    39.0    15.4
+//   2 1008 2048     2.1     2.3           2 8192 8192    15.9    14.4
+//   8 1008 2048     2.8     2.3           8 8192 8192    39.0    14.4
 bool rows_faster(const LinearI8& a) {
   const double b = (double)a.n * a.k;
   return a.m == 1 || (a.m <= 8 && 1.8 + a.m * b / 10e6 < 2.2 + b / 5e6);
 }
 // mma.sync for up to 32 rows against tcgen05 with the channels as its rows and K split over a cluster:
-//   16 1008 2048    2.8, 6.2    16 8192 8192   18.5, 23.6    32 1008 2048  4.1, 6.4
-//   32 4096 1024    3.9, 5.9    32 8192 8192   28.2, 21.5
+//   16 1008 2048    2.6, 6.2    16 8192 8192   15.4, 23.6    32 1008 2048  3.6, 6.4
+//   32 4096 1024    3.6, 5.9    32 8192 8192   28.2, 21.5
 bool few_faster(const LinearI8& a) {
   const double b = (double)a.n * a.k;
   return a.m <= 16 || (a.m <= 32 && 3.2 + b / 2.7e6 < 5.5 + b / 4.2e6);
@@ -1338,7 +1364,8 @@ Variant pick(const LinearI8& a, int sms) {
 cudaError_t launch_linear_i8(const LinearI8& a, int sms, int* status, cudaStream_t s) {
   if (rows_faster(a)) return linear_rows(a, s);
   if (few_faster(a)) {
-    // 32 channels a CTA halve the reads of x, 16 fill the SMs: 16 8192 8192 18.5, 22.1; 16 1008 2048 3.6, 2.8
+    // 32 channels a CTA halve the reads of x, 16 fill the SMs: 16 8192 8192 15.4, 18.5; 12 4096 1024 2.8, 3.4;
+    // 16 1008 2048 3.3, 2.6
     const bool wide = a.n >= 16 * sms;
     if (a.m <= 8) return linear_few<1, 1>(a, s);
     if (a.m <= 16) return wide ? linear_few<2, 2>(a, s) : linear_few<2, 1>(a, s);
