@@ -408,8 +408,8 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  * between 0.68 and 1.21 for all but the smallest.  X is held in FP32 (calls of
  * small matrices only: as two binary16 numbers, 22 bits).  The products take
  * binary16 copies of their operands, scaled by powers of two, and accumulate
- * in FP32: two copies of each, 22 bits, in the last three steps, and in every
- * step where rows or cols <= 64; one copy elsewhere.  The result is rounded
+ * in FP32: two copies of each, 22 bits, but one in the first two steps of four
+ * or more (the first of four) where rows and cols > 192.  The result is rounded
  * once.  That rounding is most of its error (2.1e-4 of the norm), unless the
  * matrix has a small rank: of rank 1, 9e-4.  A zero matrix gives zeros; a
  * matrix whose norm is not finite gives NaNs throughout.  The same call gives

@@ -1821,7 +1821,10 @@ static int ortho_run(const pf16_ortho_matrix* o, const pf16_muon_matrix* u, int3
   p.steps = steps;
   for (int i = 0; i < count; ++i) {
     OrthoMat& m = p.mat[i];
-    m.pairs_from = !m.precise ? steps : m.mb <= kOrthoPrecise ? 0 : std::max(0, steps - kOrthoPairSteps);
+    if (u)
+      m.pairs_from = m.precise ? 0 : steps;
+    else
+      m.pairs_from = m.mb <= 3 ? 0 : std::min(kOrthoSingleSteps, std::max(0, steps - 3));
   }
   p.muon = u != nullptr;
   p.nesterov = nesterov;

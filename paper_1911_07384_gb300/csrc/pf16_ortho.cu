@@ -14,7 +14,7 @@
 // 4e-4 off the exact result in the 2-norm, against 4e-2 with X kept in
 // binary16.)  The copies are scaled by powers of two so that no element
 // overflows (|X| <= 1.21, |A| <= 1.45, |B| <= 2.81) and small ones stay normal.
-// kOrthoPairSteps says where an operand is one copy and where the sum of two.
+// kOrthoSingleSteps says where an operand is one copy and where the sum of two.
 //
 // Layout.  Every matrix of the iteration is a grid of 64 x 64 binary16 blocks,
 // each 8 KB contiguous in the 128-byte-swizzled order that tcgen05.mma reads.

@@ -25,7 +25,7 @@ struct OrthoMat {
   int mb, nb;
   int part0, parts;   // its partial sums of squares
   int tall;
-  int precise;        // operands as pairs of binary16 copies, in steps from pairs_from on (kOrthoPairSteps)
+  int precise;        // operands as pairs of binary16 copies, in steps from pairs_from on (kOrthoSingleSteps)
   int pairs_from;
   int splits;         // X X^T: parts of its sum
   float scale;        // of the orthogonalised update in the weights' step
@@ -67,18 +67,19 @@ constexpr int kOrthoSumItems = 8;
 
 // Operands as the sum of two binary16 copies, the second of what the first's rounding left: the products are then
 // high by high, high by low and low by high, 22 bits of each operand for three times the work.
-//  - pf16_orthogonalize multiplies pairs in its last kOrthoPairSteps steps, so that the rounding of its result is
-//    the larger part of its error: 2.1e-4 of the norm against 1.2e-3 to 1.8e-3 with single copies throughout
-//    (1000 x 2048, tiles 256 wide: 249 us single, 345 two steps, 384 three, 438 all five; 4096 x 4096: 1046, 1659,
-//    1984, 2639; two steps leave 3.7e-4).
-//    A product's rounding weighs as b s^2 + c s^4 does, and by the third step from the end few singular values
-//    are large: what the steps before add is 1e-5 for a matrix of full rank, up to 9e-4 for one of rank 1.
+//  - pf16_orthogonalize multiplies pairs after its first kOrthoSingleSteps steps, so that the rounding of its
+//    result is the larger part of its error: 2.1e-4 of the norm against 1.2e-3 to 1.8e-3 with single copies
+//    throughout (1000 x 2048, tiles 256 wide: 249 us single, 345 two steps of pairs, 384 three, 438 all five;
+//    4096 x 4096: 1046, 1659, 1984, 2639; two of five steps leave 3.7e-4).  A product's rounding weighs as
+//    b s^2 + c s^4 does, and the singular values of a large matrix of full rank only begin to be large in the third
+//    step: what the two before add is 1e-5 from 1000 rows on, 1e-4 for 200, and up to 9e-4 for a matrix of rank 1.  Of
+//    up to 192 rows or columns (130: another 3e-4) and of three steps or fewer all are on pairs.
 //  - The optimiser step multiplies single copies: its result is a fraction lr of a weight that is rounded to
 //    binary16 itself.
 //  - Matrices of at most kOrthoPrecise blocks of rows take pairs in every step of either call.  The roundings of
 //    single copies average out over many singular values; a few singular values can each be several tenths of a
 //    percent off, and the products of so small a matrix cost nothing.
-constexpr int kOrthoPairSteps = 3;
+constexpr int kOrthoSingleSteps = 2;
 constexpr int kOrthoPrecise = 1;
 
 // A call whose matrices all have at most kOrthoPrecise blocks of rows and kSmallBlocks of columns runs in one

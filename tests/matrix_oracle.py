@@ -45,7 +45,7 @@ def orthogonal_tolerance(u, steps=5, single=5):
     draws that come out near zero.  Where the last step multiplies pairs, the emulation has 2^-22 of
     each operand; FP32 sums of 3 n / 16 instructions' products are up to 2^-24 of their
     magnitudes off at each, twice in B and once in X, and a step passes an error on at most 3.44 times
-    as large: 2^-24 (3 n / 16) times 16 covers the last three, beside 2^-12 for the steps before them."""
+    as large: 2^-24 (3 n / 16) times 16 covers the steps of pairs, beside 2^-12 for those before them."""
     e = orthogonal(u, steps)
     off = np.linalg.norm(orthogonal(u, steps, copies=single + 1) - e)
     if single < steps or min(u.shape) <= 64:
