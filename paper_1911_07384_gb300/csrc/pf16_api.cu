@@ -1702,9 +1702,9 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, bool mu
     OrthoMat& m = p->mat[i];
     const int terms = m.precise ? 3 * m.nb : m.nb;
     // X X^T's sum split so that no item is longer than a pair of SMs' share of all matrices' such products, but
-    // into no less than 16 blocks (about 4 us; the parts' store, their phase and its wait take about 8).  Three
-    // matrices of 512 x 4608 in a call take 303 us, with whole sums 330; 256 x 2304 248, 307; all filters of a
-    // ResNet-50 646, whole 630, at its own share, whatever the others', 695; with pairs of copies 742, 778, 890.
+    // into no less than 16 blocks (about 4 us; the parts' store, their phase and its wait take about 6).  Three
+    // matrices of 512 x 4608 in a call take 309 us, with whole sums 340; 256 x 2304 217, 280; all filters of a
+    // ResNet-50 597, whole 591, at its own share, whatever the others', 635; with pairs of copies 687, 728, 830.
     const long long share = std::max(16ll, products / kOrthoPairs);
     m.splits = (int)std::min<long long>(8, std::max<long long>(1, terms / share));
     const int mt = ortho_tiles(m.mb), tri = ortho_sym(mt);
@@ -1719,8 +1719,8 @@ static size_t ortho_plan(OrthoParams* p, const OrthoEntry* e, int count, bool mu
     wide += (long long)mt * cdiv(m.nb, 4);
   }
   // The full product's tiles are 256 columns wide, or 128 while every tile still has a pair of SMs for itself:
-  // one's time counts then, its product's and its epilogue's, which reads and writes X (256, 128 wide, pairs
-  // of copies: 1000 x 2048, 32 tiles of 256, 384, 358 us; single copies: there 249, 257, 512 x 512 200, 178).
+  // one's time counts then, its product's and its epilogue's, which reads and writes X (256, 128 wide:
+  // 1000 x 2048, 32 tiles of 256, 348, 330 us; 512 x 512 281, 234; 256 x 2304 258, 217).
   p->full_blocks = wide > kOrthoPairs / 2 ? 4 : 2;
   for (int i = 0; i < count; ++i) {
     p->pre_full[i] = (int)full;

@@ -28,10 +28,10 @@
 // Tiles.  A product's tile is 256 x 256, made by a pair of CTAs with
 // tcgen05.mma.cta_group::2: each CTA loads 128 rows of either operand, 64 bytes
 // a clock at the full MMA rate, where single CTAs' 128 x 128 tiles load twice
-// that (4096 x 4096, single copies: 2.34 ms with those, 1.05 with pairs).
+// that (4096 x 4096, single copies: 2.34 ms with those, 1.0 with pairs).
 // X X^T of a wide matrix has few tiles and long sums: the sum is split over n,
 // and a phase of its own, in items small enough for every SM to have one, adds
-// the parts in order (256 x 2304: 307 us whole, 248 split).
+// the parts in order (256 x 2304: 280 us whole, 217 split).
 //
 // Schedule.  After the norms and the packing, one persistent kernel runs all
 // phases of all matrices: work items (tiles of a product) are numbered phase by phase
@@ -42,10 +42,10 @@
 //
 // What bounds it.  4096 x 4096 the MMAs: 2.0 to 2.2 ms for 11/5 of 735 us of them
 // (three steps of pairs).  Smaller matrices the chain of phases, three or four
-// a step: each ends with an epilogue (6 us for a 256 x 256 tile: X read and
-// written in FP32, two binary16 stores) and 2 us of stores becoming visible and
-// counted before the next can load (1000 x 2048: 362 us; ResNet-50's 53
-// filters, single copies: 560 of a step's 646, the packing 52, the norms 30).
+// a step: each ends with an epilogue (X read and written in FP32, one or two
+// binary16 stores) and with its stores becoming visible and counted before the
+// next can load, 6 to 8 us beside the products (1000 x 2048: 330 us; ResNet-50's
+// 53 filters, single copies: 515 of a step's 600, the packing 52, the norms 30).
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -81,6 +81,10 @@ __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
   uint32_t v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
+}
+__device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
+__device__ __forceinline__ void red_add(uint32_t* p, uint32_t v) {
+  asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 __device__ __forceinline__ void red_release_add(uint32_t* p, uint32_t v) {
   asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
@@ -132,8 +136,8 @@ __device__ __forceinline__ void sym_tile(int local, int& I, int& J) {
   J = local - ortho_sym(I);
 }
 
-// Ticket -> work item, and the count of its matrix that it waits for.
-__device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, uint32_t& need) {
+// Ticket -> work item.
+__device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket) {
   Item it;
   const int n = p.count;
   const int tg = p.pre_gram[n], ta = p.pre_sum[n], ts = p.pre_sym[n], tf = p.pre_full[n];
@@ -145,7 +149,6 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
   if (it.step >= p.steps) {
     it.kind = kStop;
     it.mat = it.I = it.J = it.k1 = 0;
-    need = 0;
     return it;
   }
   if (t < (uint32_t)tg) {
@@ -182,6 +185,11 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
     it.J = local / mt;
     it.k1 = ortho_sum(p.mat[it.mat], it.step, p.mat[it.mat].mb);
   }
+  return it;
+}
+
+// The count of its matrix that an item waits for: all items of the phases before it.
+__device__ __forceinline__ uint32_t needed(const OrthoParams& p, const Item& it) {
   const OrthoMat& M = p.mat[it.mat];
   const int mt = ortho_tiles(M.mb), nt = (M.nb + p.full_blocks - 1) / p.full_blocks;
   const uint32_t tri = (uint32_t)ortho_sym(mt), gram = tri * (uint32_t)M.splits;
@@ -190,8 +198,7 @@ __device__ __forceinline__ Item decode(const OrthoParams& p, uint32_t ticket, ui
   if (it.kind != kGram) before += gram;
   if (it.kind == kSym || it.kind == kFull) before += sum;
   if (it.kind == kFull) before += tri;
-  need = kOrthoSignals * before;
-  return it;
+  return kOrthoSignals * before;
 }
 
 }  // namespace
@@ -600,10 +607,7 @@ struct TileOut {
                    make_uint4(f2h2(f[8 * h], f[8 * h + 1]), f2h2(f[8 * h + 2], f[8 * h + 3]),
                               f2h2(f[8 * h + 4], f[8 * h + 5]), f2h2(f[8 * h + 6], f[8 * h + 7])));
     if (c & 1) {
-      if (lo)
-        fence_proxy_async_all();  // the operand copies read what was stored directly
-      else
-        fence_proxy_async_smem();
+      fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         bulk_store_1d(out + (c >> 1) * (2 * kOrthoBlk), stage_w, 4096);
@@ -629,8 +633,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* staging = smem + kStages * kStageBytes;
   // (full, item_empty and acc_empty are used in the leading CTA only)
-  __shared__ uint64_t full[kStages], empty[kStages], item_full[kRing], item_empty[kRing], acc_full[2], acc_empty[2],
-      last;
+  __shared__ uint64_t full[kStages], empty[kStages], item_full[kRing], item_empty[kRing], ready[kRing],
+      acc_full[2], acc_empty[2], last;
   __shared__ Item ring[kRing];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s, drained;
@@ -644,6 +648,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&item_full[i]), 1);
+      mbar_init(smem_u32(&ready[i]), 1);
       mbar_init(smem_u32(&item_empty[i]), 1 + kEpi / 32 + 1 + kEpi / 32);  // every reader in both CTAs
     }
     for (int i = 0; i < 2; ++i) {
@@ -673,24 +678,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       while (true) {
         Item it;
         if (rank == 0) {
-          uint32_t need;
-          it = decode(p, ticket, need);
+          it = decode(p, ticket);
           if (it.kind != kStop) ticket = atomicAdd(p.ticket, 1u);  // (its latency passes behind this item)
           if (!mbar_wait_cluster(smem_u32(&item_empty[slot]), rphase ^ 1, 3 * lim)) {
             record_timeout(p.status, abort_flag);
             break;
-          }
-          if (it.kind != kStop) {
-            const uint32_t* d = p.done + it.mat;
-            if (ld_acquire(d) < need) {
-              const uint64_t t0 = globaltimer_ns();
-              while (ld_acquire(d) < need) {
-                if (*abort_flag || globaltimer_ns() - t0 > lim) {
-                  record_timeout(p.status, abort_flag);
-                  break;
-                }
-              }
-            }
           }
           if (*abort_flag) it.kind = kStop;
           ring[slot] = it;
@@ -705,15 +697,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             break;
           }
           it = ring[slot];
-          mbar_arrive_cluster(map_rank(smem_u32(&item_empty[slot]), 0));
-        }
-        if (++slot == kRing) {
-          slot = 0;
-          rphase ^= 1;
         }
         if (it.kind == kStop) break;
-        if (it.kind == kSum) continue;
-        fence_proxy_async_all();  // the blocks' writers used both proxies
         const OrthoMat& M = p.mat[it.mat];
         const OrthoLayout L = ortho_layout(M.mb, M.nb, M.splits, M.precise);
         const int base = (int)((M.ws - p.ws) >> 7);
@@ -729,6 +714,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t bytes = kOrthoBlk * (uint32_t)((it.I * 4 + 2 < M.mb ? 4 : 2) +
                                                       (same ? 0 : ((it.J * 2 + 1) * half_b < rows_b ? 2 : 1) * half_b));
         const int lo = (int)(L.lo >> 7);
+        // Each CTA waits for the item's dependency itself: handed on with the item, it would reach the other
+        // one a release later (about 1000 clocks).
+        {
+          const uint32_t need = needed(p, it);
+          const uint32_t* d = p.done + it.mat;
+          if (ld_acquire(d) < need) {
+            const uint64_t t0 = globaltimer_ns();
+            while (ld_acquire(d) < need) {
+              if (*abort_flag || globaltimer_ns() - t0 > lim) {
+                record_timeout(p.status, abort_flag);
+                break;
+              }
+            }
+          }
+        }
+        mbar_arrive(smem_u32(&ready[slot]));
+        // (relaxed, as every arrival that only says that something has been read)
+        if (rank != 0) mbar_arrive_cluster_relaxed(map_rank(smem_u32(&item_empty[slot]), 0));
+        if (*abort_flag) break;
+        if (++slot == kRing) {
+          slot = 0;
+          rphase ^= 1;
+        }
+        if (it.kind == kSum) continue;
+        // The blocks' writers used both proxies.  This fence, on the way from every store that the counter has
+        // covered to the copies, is the only one; another by the writers cost each phase about 0.7 us.
+        fence_proxy_async_all();
         for (int at = it.k0; at < it.k1 && !*abort_flag;) {
           const Run run(it, M, at);
           OperandRun a, b;
@@ -851,8 +863,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         break;
       }
       const Item it = ring[slot];
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(far_item + (uint32_t)slot * 8);
+      if (it.kind != kStop && !mbar_wait(smem_u32(&ready[slot]), rphase, 4 * lim)) record_timeout(p.status, abort_flag);
+      if (__any_sync(0xffffffffu, *abort_flag || it.step < 0)) break;  // (a step is not: the whole item has been read)
+      // (only now: the slot's next item must not pass a phase of `ready` that this warp has not seen)
+      if (lane == 0) mbar_arrive_cluster_relaxed(far_item + (uint32_t)slot * 8);
       if (++slot == kRing) {
         slot = 0;
         rphase ^= 1;
@@ -917,7 +931,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             __stcg(reinterpret_cast<uint4*>(dst + L.lo + p1), make_uint4(h[4], h[5], h[6], h[7]));
           }
         }
-        fence_proxy_async_all();  // the operand copies read them
         __syncwarp();
         if (lane == 0) red_release_add(p.done + it.mat, 1u);
         continue;
@@ -964,9 +977,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
         bulk_wait0();
-        red_release_add(p.done + it.mat, 1u);
+        fence_gpu();  // one for both signals: a release each takes as long again
+        red_add(p.done + it.mat, 1u);
+        mbar_arrive_cluster_relaxed(far_acc + (uint32_t)acc * 8);
       }
       __syncwarp();
       acc ^= 1;

@@ -69,8 +69,8 @@ constexpr int kOrthoSumItems = 8;
 // high by high, high by low and low by high, 22 bits of each operand for three times the work.
 //  - pf16_orthogonalize multiplies pairs after its first kOrthoSingleSteps steps, so that the rounding of its
 //    result is the larger part of its error: 2.1e-4 of the norm against 1.2e-3 to 1.8e-3 with single copies
-//    throughout (1000 x 2048, tiles 256 wide: 249 us single, 345 two steps of pairs, 384 three, 438 all five;
-//    4096 x 4096: 1046, 1659, 1984, 2639; two of five steps leave 3.7e-4).  A product's rounding weighs as
+//    throughout (1000 x 2048: 227 us single, 297 two steps of pairs, 330 three, 395 all five; 4096 x 4096: 998,
+//    1638, 1952, 2588; two of five steps leave 3.7e-4).  A product's rounding weighs as
 //    b s^2 + c s^4 does, and the singular values of a large matrix of full rank only begin to be large in the third
 //    step: what the two before add is 1e-5 from 1000 rows on, 1e-4 for 200, and up to 9e-4 for a matrix of rank 1.  Of
 //    up to 192 rows or columns (130: another 3e-4) and of three steps or fewer all are on pairs.
