@@ -1141,7 +1141,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       store_tile<256>(a, tacc, swb + acc * 256, staging + (warp - 1) * 4096, r0, q0, sx, lane);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(far_acc + (uint32_t)acc * 8);
+      // relaxed: the accumulator has been read and nothing is published; a release would wait for the tile's stores
+      if (lane == 0) mbar_arrive_cluster_relaxed(far_acc + (uint32_t)acc * 8);
     }
   } else if (warp <= 12) {
     const int ct = tid - 160;
@@ -1340,8 +1341,8 @@ enum Variant { V_SPLIT2, V_SPLIT4, V_BIG64, V_BIG128, V_PAIR };
 //   128 8192 8192       56.7           43.6    55.4
 //   4096 512 512        16.4 24.5      8.5      6.9     10.5
 //   512 4096 4096       54.3 62.7     41.1     28.6     35.4
-//   2048 2048 2048      62.7 74.4     41.3     29.3     21.9
-//   12544 2048 512       157  257     58.1     43.8     39.1
+//   2048 2048 2048      62.7 74.4     41.3     29.1     21.3
+//   12544 2048 512       157  257     58.1     43.7     35.1
 Variant pick(const LinearI8& a, int sms) {
   auto up = [](long long x, long long y) { return (double)((x + y - 1) / y); };
   const double ns = up(a.k, 128), kbs = up(a.k, 64), p = up(a.m, 128);
