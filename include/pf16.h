@@ -441,8 +441,8 @@ int pf16_orthogonalize(const pf16_ortho_matrix* mats, int32_t count, int32_t ste
  *   w = rn(w - lr*(scale*O(u) + wd*w)),  O(u) the result above, unrounded
  * with everything between the stored tensors in FP32, but for the products'
  * binary16 operands: one copy of each in all steps here (1.2e-3 to 1.8e-3 of
- * O's norm), two where rows or cols <= 64.  lr, momentum and wd
- * are finite floats, scale too (per matrix: often sqrt(max(1, rows/cols)))
+ * O's norm), two where rows or cols <= 64.  lr, momentum and wd are finite
+ * floats, scale too (per matrix: often sqrt(max(1, rows/cols)))
  * (PF16_ERR_ARG).  w and v overlap nothing else of the call (PF16_ERR_ARG). */
 #define PF16_MUON_NESTEROV 0x1u
 typedef struct {
@@ -474,8 +474,9 @@ int pf16_quantize_i8(const uint16_t* x, int8_t* q, float* scale, int32_t m, int3
  * or NULL.  The integer sum is exact up to k = 1024, and for any k while its
  * partial sums stay within 2^24; beyond, partial sums are FP32.  The scale
  * and the bias are applied in FP32 and the result is rounded once.  Any values
- * of x and w, -128 included.  m may be 0; n, k >= 1; m, n <= 2^30, k <= 65536.  x, w and y
- * 16-byte aligned, sx and sw 4-byte, bias 2-byte; y overlaps nothing else (PF16_ERR_ARG). */
+ * of x and w, -128 included.  m may be 0; n, k >= 1; m, n <= 2^30,
+ * k <= 65536.  x, w and y 16-byte aligned, sx and sw 4-byte, bias 2-byte; y
+ * overlaps nothing else (PF16_ERR_ARG). */
 int pf16_linear_i8(const int8_t* x, const float* sx, const int8_t* w, const float* sw, const uint16_t* bias,
                    uint16_t* y, int32_t m, int32_t n, int32_t k, void* stream);
 

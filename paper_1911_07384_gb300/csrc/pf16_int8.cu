@@ -52,24 +52,23 @@ __device__ __forceinline__ float stored_scale(float a) {
 
 }  // namespace
 
-// R rows by each group of G threads (G <= 32: part of a warp; 256: the CTA).
+// A row by each group of G threads (G <= 32: part of a warp; 256: the CTA).
 // Vectors of 8 values at multiples of 8 in the whole array, for which x's 16 bytes and q's 8 are aligned; unless VEC
 // (k a multiple of 8) a row's first and last are shared with its neighbours: their values count as zeros, and the
 // row's own integers are stored one at a time.  A thread keeps its first KEEP vectors in registers between
 // the maximum and the rounding and reads the others twice.
-// Bound by memory: every load of a thread's rows is issued before the first maximum is taken.
-template <int G, int KEEP, int R, bool VEC>
+// Bound by memory: every load of a thread's is issued before the first maximum is taken.
+template <int G, int KEEP, bool VEC>
 __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict__ x, int8_t* __restrict__ q,
                                                      float* __restrict__ scale, long long m, int k) {
   pdl_wait();
   constexpr int GROUPS = 256 / G;
   const int g = (int)threadIdx.x % G;
-  const long long row0 = (long long)blockIdx.x * (GROUPS * R) + threadIdx.x / G;  // and every GROUPS-th from there
-  // a row's first element in its first vector, and its vectors
-  auto lead = [&](long long row) { return VEC ? 0 : (int)((unsigned)(row * k) & 7u); };
-  auto vectors = [&](long long row) { return (lead(row) + k + 7) >> 3; };
-  auto load = [&](long long row, int c) {
-    const int first = lead(row);
+  const long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / G;
+  // the row's first element in its first vector, and its vectors
+  const int first = VEC ? 0 : (int)((unsigned)(row * k) & 7u);
+  const int nv = row < m ? (first + k + 7) >> 3 : 0;
+  auto load = [&](int c) {
     const long long at = row * k - first + 8ll * c;
     uint4 v;
     if (VEC || at + 8 <= m * k) {
@@ -86,116 +85,92 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
       const int i = 8 * c - first;  // of the row
       if (i < 0 || i + 8 > k) {
         auto own = [&](uint32_t h, int j) {
-          return (i + j >= 0 && i + j < k ? h & 0xffffu : 0u) | (i + j + 1 >= 0 && i + j + 1 < k ? h & 0xffff0000u : 0u);
+          return (i + j >= 0 && i + j < k ? h & 0xffffu : 0u) |
+                 (i + j + 1 >= 0 && i + j + 1 < k ? h & 0xffff0000u : 0u);
         };
         v = make_uint4(own(v.x, 0), own(v.y, 2), own(v.z, 4), own(v.w, 6));
       }
     }
     return v;
   };
-  uint4 keep[R][KEEP];
-  uint32_t mx[R];
+  uint4 keep[KEEP];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const long long row = row0 + r * GROUPS;
+  for (int i = 0; i < KEEP; ++i) keep[i] = g + i * G < nv ? load(g + i * G) : make_uint4(0, 0, 0, 0);
+  uint32_t mx = 0;
+  auto widest = [&](const uint4& v) { mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, v.x), v.y), v.z), v.w); };
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      keep[r][i] = row < m && g + i * G < vectors(row) ? load(row, g + i * G) : make_uint4(0, 0, 0, 0);
-  }
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const long long row = row0 + r * GROUPS;
-    uint32_t v = 0;
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      v = abs_max2(abs_max2(abs_max2(abs_max2(v, keep[r][i].x), keep[r][i].y), keep[r][i].z), keep[r][i].w);
-    for (int c = g + KEEP * G; c < (row < m ? vectors(row) : 0); c += G) {
-      const uint4 u = load(row, c);
-      v = abs_max2(abs_max2(abs_max2(abs_max2(v, u.x), u.y), u.z), u.w);
-    }
-    mx[r] = v;
-  }
+  for (int i = 0; i < KEEP; ++i) widest(keep[i]);
+  for (int c = g + KEEP * G; c < nv; c += G) widest(load(c));
   constexpr int W = G < 32 ? G : 32;
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1)
-#pragma unroll
-    for (int r = 0; r < R; ++r) mx[r] = abs_max2(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], o));
-#pragma unroll
-  for (int r = 0; r < R; ++r) mx[r] = abs_max2(mx[r], mx[r] >> 16);
+  for (int o = W / 2; o > 0; o >>= 1) mx = abs_max2(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  mx = abs_max2(mx, mx >> 16);
   if (G > 32) {
-    __shared__ uint32_t red[R][8];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if ((threadIdx.x & 31) == 0) red[r][threadIdx.x >> 5] = mx[r];
+    __shared__ uint32_t red[8];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mx;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) mx[r] = abs_max2(mx[r], red[r][i]);
+    for (int i = 0; i < 8; ++i) mx = abs_max2(mx, red[i]);
   }
+  if (row >= m) return;
+  const float a = h2f((uint16_t)mx);
+  const RowScale s = row_scale(a);
+  if (g == 0) scale[row] = stored_scale(a);
+  // with r = 0 (a zero row, or one that is not finite) the integers are zero
+  auto put = [&](int c, const uint4& v) {
+    const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+    uint2 o = make_uint2(0, 0);
+    if (s.r != 0.f) {
+      uint32_t b[8];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const long long row = row0 + r * GROUPS;
-    if (row >= m) break;
-    const float a = h2f((uint16_t)mx[r]);
-    const RowScale s = row_scale(a);
-    if (g == 0) scale[row] = stored_scale(a);
-    // with r = 0 (a zero row, or one that is not finite) the integers are zero
-    auto put = [&](int c, const uint4& v) {
-      const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-      uint2 o = make_uint2(0, 0);
-      if (s.r != 0.f) {
-        uint32_t b[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          b[2 * j] = quant1((uint16_t)h[j], s);
-          b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
-        }
-        o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
-        o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
+      for (int j = 0; j < 4; ++j) {
+        b[2 * j] = quant1((uint16_t)h[j], s);
+        b[2 * j + 1] = quant1((uint16_t)(h[j] >> 16), s);
       }
-      const int i = 8 * c - lead(row);
-      int8_t* at = q + row * k + i;
-      if (VEC || (i >= 0 && i + 8 <= k)) {
-        __stcs(reinterpret_cast<uint2*>(at), o);
-      } else {
+      o.x = prmt(prmt(b[0], b[1], 0x0040), prmt(b[2], b[3], 0x0040), 0x5410);
+      o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
+    }
+    const int i = 8 * c - first;
+    int8_t* at = q + row * k + i;
+    if (VEC || (i >= 0 && i + 8 <= k)) {
+      __stcs(reinterpret_cast<uint2*>(at), o);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (i + j >= 0 && i + j < k) at[j] = (int8_t)((j < 4 ? o.x : o.y) >> ((j & 3) * 8));
-      }
-    };
-    const int nv = vectors(row);
+      for (int j = 0; j < 8; ++j)
+        if (i + j >= 0 && i + j < k) at[j] = (int8_t)((j < 4 ? o.x : o.y) >> ((j & 3) * 8));
+    }
+  };
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-      if (g + i * G < nv) put(g + i * G, keep[r][i]);
-    for (int c = g + KEEP * G; c < nv; c += G) put(c, load(row, c));
-  }
+  for (int i = 0; i < KEEP; ++i)
+    if (g + i * G < nv) put(g + i * G, keep[i]);
+  for (int c = g + KEEP * G; c < nv; c += G) put(c, load(c));
 }
 
-template <int G, int KEEP, int R>
+template <int G, int KEEP>
 static cudaError_t quantize_g(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s) {
-  const long long rows = 256 / G * R;
+  constexpr long long rows = 256 / G;
   const dim3 grid((unsigned)((m + rows - 1) / rows)), block(256);
   const cudaError_t e = (k & 7) == 0
-                            ? launch_pdl(k_quantize_i8<G, KEEP, R, true>, grid, block, 0, s, x, q, scale, m, k)
-                            : launch_pdl(k_quantize_i8<G, KEEP, R, false>, grid, block, 0, s, x, q, scale, m, k);
+                            ? launch_pdl(k_quantize_i8<G, KEEP, true>, grid, block, 0, s, x, q, scale, m, k)
+                            : launch_pdl(k_quantize_i8<G, KEEP, false>, grid, block, 0, s, x, q, scale, m, k);
   return e == cudaSuccess ? counted_launches(1) : e;
 }
 
 cudaError_t launch_quantize_i8(const uint16_t* x, int8_t* q, float* scale, long long m, int k, cudaStream_t s) {
   // Few lanes a row and four vectors a lane: what a row costs apart from its elements (its reduction and two
-  // divisions, by all its lanes) took longer than memory with a warp a row (802816 x 256: 130 us, 89 with eight lanes).  A CTA a row from 2049
-  // values on, and for few rows: 2000 x 2048 4.2 us by warps, 4.2 by CTAs; 12544 x 2048 13.9, 18.7 (four rows a CTA);
-  // 4096 x 4096 11.4, 10.6.
+  // divisions, by all its lanes) took longer than memory with a warp a row (802816 x 256: 130 us, 89 with eight
+  // lanes).  A CTA a row from 2049 values on, and for few rows (by warps, by CTAs: 2000 x 2048 4.2, 4.2 us;
+  // 12544 x 2048 13.9, 18.7; 184147 x 1065 156, 297; 4096 x 4096 11.4, 10.6).
   const int n = (k & 7) == 0 ? k : (k + 14) / 8 * 8;  // values in a row's vectors, at most
-  if (n <= 64) return quantize_g<2, 4, 1>(x, q, scale, m, k, s);
-  if (n <= 128) return quantize_g<4, 4, 1>(x, q, scale, m, k, s);
-  if (n <= 256) return quantize_g<8, 4, 1>(x, q, scale, m, k, s);
-  if (n <= 512) return quantize_g<16, 4, 1>(x, q, scale, m, k, s);
-  if (n <= 1024) return quantize_g<32, 4, 1>(x, q, scale, m, k, s);
-  if (n <= 2048) return m < 2048 ? quantize_g<256, 1, 1>(x, q, scale, m, k, s) : quantize_g<32, 8, 1>(x, q, scale, m, k, s);
-  if (n <= 4096) return quantize_g<256, 2, 1>(x, q, scale, m, k, s);
-  return quantize_g<256, 8, 1>(x, q, scale, m, k, s);
+  if (n <= 64) return quantize_g<2, 4>(x, q, scale, m, k, s);
+  if (n <= 128) return quantize_g<4, 4>(x, q, scale, m, k, s);
+  if (n <= 256) return quantize_g<8, 4>(x, q, scale, m, k, s);
+  if (n <= 512) return quantize_g<16, 4>(x, q, scale, m, k, s);
+  if (n <= 1024) return quantize_g<32, 4>(x, q, scale, m, k, s);
+  if (n <= 2048)
+    return m < 2048 ? quantize_g<256, 1>(x, q, scale, m, k, s) : quantize_g<32, 8>(x, q, scale, m, k, s);
+  if (n <= 4096) return quantize_g<256, 2>(x, q, scale, m, k, s);
+  return quantize_g<256, 8>(x, q, scale, m, k, s);
 }
 
 // ---------------------------------------------------------------------------

@@ -113,7 +113,9 @@ __device__ __forceinline__ uint32_t low2(float x, float y, uint32_t h) {
 }
 // whether a step multiplies pairs of binary16 copies, and the blocks in its sum over n: three times as many then
 __device__ __forceinline__ bool ortho_pairs(const OrthoMat& M, int step) { return step >= M.pairs_from; }
-__device__ __forceinline__ int ortho_sum(const OrthoMat& M, int step, int n) { return ortho_pairs(M, step) ? 3 * n : n; }
+__device__ __forceinline__ int ortho_sum(const OrthoMat& M, int step, int n) {
+  return ortho_pairs(M, step) ? 3 * n : n;
+}
 
 // the largest i with pre[i] <= t, pre[0] = 0 and t < pre[n]
 __device__ __forceinline__ int find_mat(const int* pre, int n, int t) {
@@ -744,8 +746,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int at = it.k0; at < it.k1 && !*abort_flag;) {
           const Run run(it, M, at);
           OperandRun a, b;
-          a.start((it.kind == kGram ? X : S) + (run.part == 2 ? lo : 0), it.kind == kGram ? ne : me, ra, run.kb, run.a_mn, la);
-          b.start((it.kind == kSym ? S : X) + (run.part == 1 ? lo : 0), it.kind == kSym ? me : ne, rb, run.kb, run.b_mn, lb);
+          a.start((it.kind == kGram ? X : S) + (run.part == 2 ? lo : 0), it.kind == kGram ? ne : me, ra, run.kb,
+                  run.a_mn, la);
+          b.start((it.kind == kSym ? S : X) + (run.part == 1 ? lo : 0), it.kind == kSym ? me : ne, rb, run.kb,
+                  run.b_mn, lb);
           for (int kb = run.kb; at < run.end; ++at, ++kb) {
             if (!mbar_wait(smem_u32(&empty[stage]), phase ^ 1, 3 * lim)) {
               record_timeout(p.status, abort_flag);
@@ -814,8 +818,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const bool a_mn = run.a_mn, b_mn = run.b_mn;
           const uint64_t ad0 = a_mn ? mndesc : kdesc, bd0 = (b_mn ? mndesc : kdesc) + (same ? 0 : 2 * kOrthoBlk >> 4);
           const uint32_t as = a_mn ? 2048 >> 4 : 32 >> 4, bs = b_mn ? 2048 >> 4 : 32 >> 4;
-          const uint32_t idesc = (it.kind == kFull ? idesc_full : idesc_f16(256, 256, false, false, true)) | (a_mn ? 1u << 15 : 0u) |
-                                 (b_mn ? 1u << 16 : 0u);
+          const uint32_t idesc = (it.kind == kFull ? idesc_full : idesc_f16(256, 256, false, false, true)) |
+                                 (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
           for (; at < run.end; ++at) {
             if (!mbar_wait_cluster(smem_u32(&full[stage]), phase, 2 * lim)) {
               record_timeout(p.status, abort_flag);
