@@ -67,12 +67,16 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
   const long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / G;
   // the row's first element in its first vector, and its vectors
   const int first = VEC ? 0 : (int)((unsigned)(row * k) & 7u);
-  const int nv = row < m ? (first + k + 7) >> 3 : 0;
+  const int nv = VEC ? k >> 3 : (first + k + 7) >> 3;
+  const bool live = row < m;
+  const uint4* const xv = reinterpret_cast<const uint4*>(x + (row * k - first));
+  uint2* const qv = reinterpret_cast<uint2*>(q + (row * k - first));
   auto load = [&](int c) {
+    if (VEC) return __ldcs(xv + c);
     const long long at = row * k - first + 8ll * c;
     uint4 v;
-    if (VEC || at + 8 <= m * k) {
-      v = __ldcs(reinterpret_cast<const uint4*>(x + at));
+    if (at + 8 <= m * k) {
+      v = __ldcs(xv + c);
     } else {  // the array's last
       uint32_t h[4];
 #pragma unroll
@@ -95,12 +99,12 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
   };
   uint4 keep[KEEP];
 #pragma unroll
-  for (int i = 0; i < KEEP; ++i) keep[i] = g + i * G < nv ? load(g + i * G) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < KEEP; ++i) keep[i] = live && g + i * G < nv ? load(g + i * G) : make_uint4(0, 0, 0, 0);
   uint32_t mx = 0;
   auto widest = [&](const uint4& v) { mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, v.x), v.y), v.z), v.w); };
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) widest(keep[i]);
-  for (int c = g + KEEP * G; c < nv; c += G) widest(load(c));
+  for (int c = g + KEEP * G; c < (live ? nv : 0); c += G) widest(load(c));
   constexpr int W = G < 32 ? G : 32;
 #pragma unroll
   for (int o = W / 2; o > 0; o >>= 1) mx = abs_max2(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -112,7 +116,7 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
 #pragma unroll
     for (int i = 0; i < 8; ++i) mx = abs_max2(mx, red[i]);
   }
-  if (row >= m) return;
+  if (!live) return;
   const float a = h2f((uint16_t)mx);
   const RowScale s = row_scale(a);
   if (g == 0) scale[row] = stored_scale(a);
@@ -131,10 +135,10 @@ __global__ void __launch_bounds__(256) k_quantize_i8(const uint16_t* __restrict_
       o.y = prmt(prmt(b[4], b[5], 0x0040), prmt(b[6], b[7], 0x0040), 0x5410);
     }
     const int i = 8 * c - first;
-    int8_t* at = q + row * k + i;
     if (VEC || (i >= 0 && i + 8 <= k)) {
-      __stcs(reinterpret_cast<uint2*>(at), o);
+      __stcs(qv + c, o);
     } else {
+      int8_t* at = reinterpret_cast<int8_t*>(qv + c);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (i + j >= 0 && i + j < k) at[j] = (int8_t)((j < 4 ? o.x : o.y) >> ((j & 3) * 8));
