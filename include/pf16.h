@@ -410,10 +410,11 @@ int pf16_softmax_xent(const uint16_t* logits, const uint16_t* bias, const int32_
  * binary16 copies of their operands, scaled by powers of two, and accumulate
  * in FP32: two copies of each, 22 bits, but one in the first two steps of four
  * or more (the first of four) where rows and cols > 192.  The result is rounded
- * once.  That rounding is most of its error (2.1e-4 of the norm), unless the
- * matrix has a small rank: of rank 1, 9e-4.  A zero matrix gives zeros; a
- * matrix whose norm is not finite gives NaNs throughout.  The same call gives
- * the same bits.
+ * once.  That rounding is most of its error (2.1e-4 of the norm) for up to
+ * eight steps, unless the matrix has a small rank (of rank 1, 9e-4); each
+ * further step carries FP32's own roundings up to 1.6 times as far.  A zero
+ * matrix gives zeros; a matrix whose norm is not finite gives NaNs throughout.
+ * The same call gives the same bits.
  *
  * All matrices of one call run together, in three launches, or in one where
  * each has a side of at most 64 and the other of at most 704.  1 <= rows,
@@ -441,7 +442,7 @@ int pf16_orthogonalize(const pf16_ortho_matrix* mats, int32_t count, int32_t ste
  *   w = rn(w - lr*(scale*O(u) + wd*w)),  O(u) the result above, unrounded
  * with everything between the stored tensors in FP32, but for the products'
  * binary16 operands: one copy of each in all steps here (1.2e-3 to 1.8e-3 of
- * O's norm), two where rows or cols <= 64.  lr, momentum and wd are finite
+ * O's norm after five), two where rows or cols <= 64.  lr, momentum and wd are finite
  * floats, scale too (per matrix: often sqrt(max(1, rows/cols)))
  * (PF16_ERR_ARG).  w and v overlap nothing else of the call (PF16_ERR_ARG). */
 #define PF16_MUON_NESTEROV 0x1u
